@@ -92,7 +92,8 @@ enum {
   FAAR_OP_ATTENTION_FWD = 10, /* faar_workspace_bytes(op, O = n_q * dh, K = n_kv * dh, T = tokens, 0) */
   FAAR_OP_ATTENTION_BWD = 11, /* likewise */
   FAAR_OP_GRAM_PREPARE = 12,  /* faar_workspace_bytes(op, O = K, K, T, 0) */
-  FAAR_OP_LAYER_STEP_GRAM = 13 /* faar_workspace_bytes(op, O, K, T = 1, 0) */
+  FAAR_OP_LAYER_STEP_GRAM = 13, /* faar_workspace_bytes(op, O, K, T = 1, 0) */
+  FAAR_OP_LAYERNORM_BWD = 14  /* faar_workspace_bytes(op, O = D (row length), K = 16, T = rows, 0) */
 };
 
 /* kernels of the path, for faar_time_kernel */
@@ -625,6 +626,42 @@ size_t faar_block_workspace_bytes(const faar_block* blk);
 int faar_block_joint_step(const faar_block* blk, const void* x, const void* y_fp, float mse_scale, float beta,
                           float lambda_round, const faar_adam* opt, float* block_loss, void* dx, void* ws, size_t ws_bytes,
                           void* stream);
+
+/*
+ * The same places in blocks that are built otherwise: layer norm for RMSNorm, rotary embedding over several position axes, and
+ * attention with capped or biased scores under document, prefix, window and whole-sequence masks.  A joint step of such a block is
+ * the sequence of calls above with these in their places (faar_block_joint_step is for the blocks above alone).
+ */
+
+/* Layer norm: h[t, i] = (x[t, i] - mean[t]) rstd[t] g[i] + b[i],  mean[t] = mean_i x[t, i],
+ * rstd[t] = 1 / sqrt(mean_i (x[t, i] - mean[t])^2 + eps).
+ *   x in [T*D] of dtype xdt; g in float[D]; b in, nullable float[D] (NULL: 0); h out bf16 [T*D]; mean, rstd out float[T] (kept for
+ *   the backward).  D % 8 == 0, D <= 16384. */
+int faar_layernorm_fwd(const void* x, faar_dtype xdt, int64_t T, int64_t D, const float* g, const float* b, float eps, void* h, float* mean,
+                       float* rstd, void* stream);
+
+/* With xh = (x - mean) rstd and dh = dh1 + dh2 + dh3:
+ *   dx = rstd (g dh - mean_i(g dh) - xh mean_i(g dh xh)) + d_res;   dg[i] = sum_t dh[t, i] xh[t, i];   db[i] = sum_t dh[t, i]
+ *   dh1 in bf16 [T*D]; dh2, dh3, d_res in, nullable bf16 [T*D] as in faar_rmsnorm_bwd; dx out bf16 [T*D];
+ *   dg, db out, nullable float[D]: summed in float32 in a fixed order (NULL where the norm is frozen).
+ *   ws: FAAR_OP_LAYERNORM_BWD, needed where dg or db is wanted. */
+int faar_layernorm_bwd(const void* dh1, const void* dh2, const void* dh3, const void* x, faar_dtype xdt, int64_t T, int64_t D,
+                       const float* g, const float* mean, const float* rstd, const void* d_res, void* dx, float* dg, float* db, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* Rotary position embedding over several position axes, of q and k in one call: frequency i < rot / 2 of every head turns by the angle
+ * pos[axis[i] * T + t] * freq[i] (radians), taken in 64 bits, so that far positions keep their phase:
+ *   y[a] = x[a] cos - x[b] sin,  y[b] = x[b] cos + x[a] sin;   (a, b) = (i, i + rot/2), with FAAR_ROPE_PAIRS (2 i, 2 i + 1).
+ * Entries rot .. dh-1 of a head are not rotated (copied, where y is not x).  FAAR_ROPE_INVERSE turns by the opposite angle: the
+ * backward pass.
+ *   q in bf16 [T][n_q * dh], row t at q + t * ldq (elements; a multiple of 8); k likewise, nullable (with yk); outputs alike, each may
+ *   be its input (with the same row stride) but must not overlap it otherwise.
+ *   pos in int32 [n_axes][T], any values; axis HOST uint8 [rot/2], values < n_axes; freq HOST double [rot/2], finite: both read
+ *   during the call.  dh % 8 == 0, dh <= 256; rot % 16 == 0. */
+enum { FAAR_ROPE_PAIRS = 1, FAAR_ROPE_INVERSE = 2 };
+int faar_rope_axes(const void* q, int64_t ldq, int64_t n_q, const void* k, int64_t ldk, int64_t n_k, int64_t T, int64_t dh, int64_t rot,
+                   const int32_t* pos, int64_t n_axes, const uint8_t* axis, const double* freq, uint32_t flags, void* yq, int64_t ldyq,
+                   void* yk, int64_t ldyk, void* stream);
 
 /* a = SiLU(p) q = p sigmoid(p) q, all bf16 [n], n % 8 == 0 */
 int faar_silu_mul_fwd(const void* p, const void* q, int64_t n, void* a, void* stream);

@@ -244,3 +244,92 @@ def attn_block_step(x, g_norm, eps, layers, n_seq, n_q, n_kv, dh, cos, sin, beta
     out["dx"] = st(rmsnorm_backward(dh_sum, x, g_norm, r) + dy)
     out.update({"do": do, "dq": dq2, "dk": dk2, "dv": dv, "dq0": dq0, "dk0": dk0})
     return out
+
+
+# ---- blocks built otherwise: layer norm, several position axes, masked attention ---------------------------------------
+def layernorm(x, g, b, eps):
+    """h = (x - mean) / sqrt(var + eps) g + b per row, the variance about the mean.  -> (h, mean, 1 / sqrt(var + eps))."""
+    x = np.asarray(x, dtype=np.float64)
+    mean = x.mean(axis=-1, keepdims=True)
+    r = 1.0 / np.sqrt(((x - mean) ** 2).mean(axis=-1, keepdims=True) + float(eps))
+    h = (x - mean) * r * np.asarray(g, dtype=np.float64)
+    return h + (0.0 if b is None else np.asarray(b, dtype=np.float64)), mean[..., 0], r[..., 0]
+
+
+def layernorm_backward(dh, x, g, mean, r):
+    """(dL/dx, dL/dg, dL/db) of h = layernorm(x, g, b):  with xh = (x - mean) r, the mean and the norm both depend on x, so that
+    dx = r (g dh - mean(g dh) - xh mean(g dh xh))."""
+    x, dh = (np.asarray(t, dtype=np.float64) for t in (x, dh))
+    r = np.asarray(r, dtype=np.float64)[..., None]
+    xh = (x - np.asarray(mean, dtype=np.float64)[..., None]) * r
+    gd = np.asarray(g, dtype=np.float64) * dh
+    dx = r * (gd - gd.mean(axis=-1, keepdims=True) - xh * (gd * xh).mean(axis=-1, keepdims=True))
+    return dx, (dh * xh).sum(axis=0), dh.sum(axis=0)
+
+
+def rope_axes(x, pos, axis, freq, dh, pairs=False, inverse=False):
+    """Rotate every head of x [T, H*dh]: frequency i turns by pos[axis[i], t] * freq[i]; it pairs entries (i, i + rot/2), or neighbours."""
+    x = np.asarray(x, dtype=np.float64)
+    T, half = x.shape[0], len(freq)
+    angle = np.asarray(pos).astype(np.longdouble)[np.asarray(axis, dtype=int)].T * np.asarray(freq, dtype=np.longdouble)
+    z = np.cos(angle).astype(np.float64) + 1j * (-1.0 if inverse else 1.0) * np.sin(angle).astype(np.float64)
+    y = x.reshape(T, -1, dh).copy()
+    a, b = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if pairs else (slice(0, half), slice(half, 2 * half))
+    w = (y[..., a] + 1j * y[..., b]) * z[:, None, :]
+    y[..., a], y[..., b] = w.real, w.imag
+    return y.reshape(T, -1)
+
+
+def allowed_keys(q_len, k_len, causal=True, prefix=0, window=0):
+    """Which keys of a sequence each of its queries sees, [q_len, k_len].  The queries are the last positions: query i stands at
+    k_len - q_len + i."""
+    p = np.arange(q_len)[:, None] + (k_len - q_len)
+    j = np.arange(k_len)[None, :]
+    ok = np.ones((q_len, k_len), dtype=bool)
+    if causal:
+        ok &= (j <= p) | (j < prefix)
+    if window:
+        ok &= np.abs(p - j) < window
+    return ok
+
+
+def masked_attention(q, k, v, seqs, n_q, n_kv, dh, scale, causal=True, window=0, cap=0.0, slopes=None, d_o=None):
+    """Attention over sequences given as (q_start, q_len, k_start, k_len, prefix), rows of q [Tq, n_q*dh] and of k, v [Tk, n_kv*dh]:
+
+        z = scale q . k;   s = cap tanh(z / cap) - slope_head |p - j|   (cap 0: s = z - ...);   P = softmax of s over the allowed keys
+        o = P v;  a query that sees no key has o = 0 and lse = -inf
+
+    -> (o, lse [n_q, Tq] (NaN for rows of no sequence)), and with d_o also (dq, dk, dv):
+        dv = P^T do;  ds = P (do v^T - sum_j P (do v^T));  dz = ds (1 - tanh^2);  dq = scale dz k;  dk = scale dz^T q."""
+    q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
+    rep = n_q // n_kv
+    o, lse = np.zeros_like(q), np.full((n_q, q.shape[0]), np.nan)
+    dq, dk, dv = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v)
+    for qs, ql, ks, kl, prefix in seqs:
+        ok = allowed_keys(ql, kl, causal, prefix, window)
+        gap = np.abs(np.arange(ql)[:, None] + (kl - ql) - np.arange(kl)[None, :])
+        for h in range(n_q):
+            cq, ck = slice(h * dh, (h + 1) * dh), slice(h // rep * dh, (h // rep + 1) * dh)
+            qh, kh, vh = q[qs:qs + ql, cq], k[ks:ks + kl, ck], v[ks:ks + kl, ck]
+            z = qh @ kh.T * scale
+            th = np.tanh(z / cap) if cap else None
+            s = (th * cap if cap else z) - (0.0 if slopes is None else float(slopes[h])) * gap
+            s = np.where(ok, s, -np.inf)
+            m = np.where(ok.any(axis=1), s.max(axis=1, initial=-np.inf), 0.0)
+            e = np.exp(s - m[:, None])
+            l = e.sum(axis=1)
+            with np.errstate(divide="ignore"):
+                lse[h, qs:qs + ql] = m + np.log(l)
+            P = e / np.where(l > 0, l, 1.0)[:, None]
+            o[qs:qs + ql, cq] = P @ vh
+            if d_o is None:
+                continue
+            do = np.asarray(d_o, dtype=np.float64)[qs:qs + ql, cq]
+            dp = do @ vh.T
+            ds = P * (dp - (P * dp).sum(axis=1, keepdims=True))
+            if cap:
+                ds = ds * (1.0 - th * th)
+            dq[qs:qs + ql, cq] = scale * (ds @ kh)
+            dk[ks:ks + kl, ck] += scale * (ds.T @ qh)
+            dv[ks:ks + kl, ck] += P.T @ do
+    return (o, lse) if d_o is None else (o, lse, dq, dk, dv)

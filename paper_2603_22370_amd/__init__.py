@@ -7,4 +7,5 @@ from .binding import (FaarError, faar_adam, faar_harden_pack, faar_hardened_loss
                       faar_softquant_fwd_bwd_static, faar_gemm_plan, tensor_batch, faar_quant_rtn_batch,
                       faar_init_v_batch, faar_harden_pack_batch, faar_linear_forward, faar_rmsnorm_fwd, faar_rmsnorm_bwd,
                       faar_silu_mul_fwd, faar_silu_mul_bwd, faar_block_output_loss, faar_residual_add, faar_rope, block_description, faar_block_workspace, faar_block_joint_step, faar_attention_fwd, faar_attention_bwd,
+                      faar_layernorm_fwd, faar_layernorm_bwd, layernorm_workspace, faar_rope_axes,
                       faar_stage2_losses, faar_workspace_bytes, layer_step_workspace, lib)

@@ -17,7 +17,7 @@ FAAR_SGLOBAL_GIVEN, FAAR_EMIT_DELTA, FAAR_WS_CHAINED, FAAR_WS_FORWARD_READY, FAA
 FAAR_WS_GRADIENT_CONSTANT = 32
 FAAR_STEP_JOINT = 64
 FAAR_STEP_WHOLE_DEVICE = 256
-OP_QUANT_RTN, OP_INIT_V, OP_SOFTQUANT, OP_LAYER_PREPARE, OP_LAYER_STEP, OP_HARDEN_PACK, OP_STAGE2_LOSSES, OP_QUANT_RTN_BATCH, OP_LINEAR_FORWARD, OP_BLOCK_OUTPUT_LOSS, OP_ATTENTION_FWD, OP_ATTENTION_BWD, OP_GRAM_PREPARE, OP_LAYER_STEP_GRAM = range(14)
+OP_QUANT_RTN, OP_INIT_V, OP_SOFTQUANT, OP_LAYER_PREPARE, OP_LAYER_STEP, OP_HARDEN_PACK, OP_STAGE2_LOSSES, OP_QUANT_RTN_BATCH, OP_LINEAR_FORWARD, OP_BLOCK_OUTPUT_LOSS, OP_ATTENTION_FWD, OP_ATTENTION_BWD, OP_GRAM_PREPARE, OP_LAYER_STEP_GRAM, OP_LAYERNORM_BWD = range(15)
 ERRORS = {-1: "FAAR_E_NULL", -2: "FAAR_E_SHAPE", -3: "FAAR_E_DTYPE", -4: "FAAR_E_WORKSPACE",
           -5: "FAAR_E_HIP", -6: "FAAR_E_ARG", -7: "FAAR_E_UNSUPPORTED"}
 
@@ -145,6 +145,14 @@ def lib() -> ctypes.CDLL:
                                          c_int64, c_int64, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         L.faar_rmsnorm_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_void_p]
+        L.faar_layernorm_fwd.restype = c_int
+        L.faar_layernorm_fwd.argtypes = [c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.faar_layernorm_bwd.restype = c_int
+        L.faar_layernorm_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.faar_rope_axes.restype = c_int
+        L.faar_rope_axes.argtypes = [c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int64, c_int64, c_void_p, c_int64,
+                                     c_void_p, c_void_p, c_uint32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
         L.faar_silu_mul_fwd.restype = c_int
         L.faar_silu_mul_fwd.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
         L.faar_silu_mul_bwd.restype = c_int
@@ -189,6 +197,18 @@ def _dev(*ts):
     for t in ts:
         if t is not None and (not t.is_cuda or not t.is_contiguous()):
             raise ValueError("tensors must be contiguous device tensors")
+
+
+def _rows(where, **ts):
+    """Device tensors [rows, width] whose rows may lie further apart than they are wide."""
+    for name, t in ts.items():
+        if t is not None and (not t.is_cuda or t.dim() != 2 or t.dtype != torch.bfloat16 or (t.shape[1] > 1 and t.stride(1) != 1)):
+            raise ValueError(f"{where}: {name} must be a bf16 device tensor [rows, width] with contiguous rows")
+
+
+def _ld(t):
+    """Elements between the starts of neighbouring rows (0: absent)."""
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
 def _check(rc: int, where: str):
@@ -536,6 +556,66 @@ def faar_rope(x, n_heads, cos_t, sin_t, inverse=False, out=None):
     _check(lib().faar_rope(_ptr(x), T, n_heads, 2 * half, _ptr(cos_t), _ptr(sin_t), S, int(bool(inverse)), _ptr(y), _stream()),
            "faar_rope")
     return y
+
+
+def faar_layernorm_fwd(x, g, b=None, eps=1e-5):
+    """Layer norm.  -> (h bf16 [T, D], mean f32 [T], rstd f32 [T])."""
+    _dev(x, g, b)
+    T, D = x.shape
+    if any(t is not None and (t.dtype != torch.float32 or t.numel() != D) for t in (g, b)):
+        raise ValueError("faar_layernorm_fwd: g, b float32 [D]")
+    h = torch.empty((T, D), dtype=torch.bfloat16, device=x.device)
+    mean, rstd = torch.empty((2, T), dtype=torch.float32, device=x.device)
+    _check(lib().faar_layernorm_fwd(_ptr(x), _dt(x), T, D, _ptr(g), _ptr(b), float(eps), _ptr(h), _ptr(mean), _ptr(rstd), _stream()),
+           "faar_layernorm_fwd")
+    return h, mean, rstd
+
+
+def layernorm_workspace(T, D, device="cuda"):
+    """A workspace for faar_layernorm_bwd calls that return weight or bias gradients."""
+    return _workspace(OP_LAYERNORM_BWD, D, 16, T, device=device)
+
+
+def faar_layernorm_bwd(dh1, x, g, mean, rstd, dh2=None, d_res=None, dh3=None, want_dg=False, want_db=False, ws=None):
+    """-> (dx bf16 [T, D], dg f32 [D] or None, db f32 [D] or None)."""
+    _dev(dh1, dh2, dh3, x, g, mean, rstd, d_res, ws)
+    T, D = x.shape
+    if any(t is not None and (t.dtype != torch.bfloat16 or t.shape != x.shape) for t in (dh1, dh2, dh3, d_res)):
+        raise ValueError("faar_layernorm_bwd: gradients are bf16 [T, D]")
+    if any(t.dtype != torch.float32 or t.numel() != n for t, n in ((g, D), (mean, T), (rstd, T))):
+        raise ValueError("faar_layernorm_bwd: g float32 [D], mean and rstd float32 [T]")
+    dx = torch.empty((T, D), dtype=torch.bfloat16, device=x.device)
+    dg, db = (torch.empty(D, dtype=torch.float32, device=x.device) if w else None for w in (want_dg, want_db))
+    if ws is None and (want_dg or want_db):
+        ws = layernorm_workspace(T, D, device=x.device)
+    _check(lib().faar_layernorm_bwd(_ptr(dh1), _ptr(dh2), _ptr(dh3), _ptr(x), _dt(x), T, D, _ptr(g), _ptr(mean), _ptr(rstd), _ptr(d_res),
+                                    _ptr(dx), _ptr(dg), _ptr(db), _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
+           "faar_layernorm_bwd")
+    return dx, dg, db
+
+
+FAAR_ROPE_PAIRS, FAAR_ROPE_INVERSE = 1, 2
+
+
+def faar_rope_axes(q, k, n_q, n_k, dh, pos, axis, freq, pairs=False, inverse=False, out=None):
+    """Rotary embedding over several position axes.  q bf16 [T, n_q * dh], k bf16 [T, n_k * dh] or None (rows may lie apart: slices of a
+    fused projection); pos int32 [n_axes, T]; axis, freq: sequences of the position axis and the frequency (radians per position) of each
+    rotated pair, len(freq) = rot / 2.  out: (yq, yk), which may be q and k.  -> (yq, yk)."""
+    yq, yk = (torch.empty((q.shape[0], q.shape[1]), dtype=q.dtype, device=q.device),
+              None if k is None else torch.empty((k.shape[0], k.shape[1]), dtype=k.dtype, device=k.device)) if out is None else out
+    _rows("faar_rope_axes", q=q, k=k, yq=yq, yk=yk)
+    _dev(pos)
+    T, half = q.shape[0], len(freq)
+    if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != T or len(axis) != half:
+        raise ValueError("faar_rope_axes: pos int32 [n_axes, T], one axis for each frequency")
+    if q.shape[1] != n_q * dh or yq.shape != q.shape or (k is None) != (yk is None) or \
+            (k is not None and (k.shape != (T, n_k * dh) or yk.shape != k.shape)):
+        raise ValueError("faar_rope_axes: q [T, n_q * dh], k [T, n_k * dh], outputs alike")
+    ax, fr = (ctypes.c_uint8 * max(half, 1))(*axis), (ctypes.c_double * max(half, 1))(*freq)
+    _check(lib().faar_rope_axes(_ptr(q), _ld(q), n_q, _ptr(k), _ld(k), n_k, T, dh, 2 * half, _ptr(pos), pos.shape[0], ax, fr,
+                                (FAAR_ROPE_PAIRS if pairs else 0) | (FAAR_ROPE_INVERSE if inverse else 0), _ptr(yq), _ld(yq), _ptr(yk),
+                                _ld(yk), _stream()), "faar_rope_axes")
+    return yq, yk
 
 
 def faar_attention_fwd(q, k, v, n_seq, n_q, n_kv, scale=None, ws=None):

@@ -49,6 +49,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255);
 
 // Largest tensor / activation extents accepted: index arithmetic is 64-bit, grids are 32-bit.
 constexpr int64_t kMaxElems = (int64_t)1 << 36;
+constexpr int64_t kLayerNormMaxD = 16384;   // a row is held in the registers of one workgroup
 
 int check_shape(int64_t O, int64_t K) {
   if (O <= 0 || K <= 0 || K % 16 != 0) return FAAR_E_SHAPE;
@@ -312,6 +313,9 @@ size_t faar_workspace_bytes(int op, int64_t O, int64_t K, int64_t T, uint32_t fl
     case FAAR_OP_BLOCK_OUTPUT_LOSS:         // O = D (row length), T rows
       if (T <= 0 || O % 8 != 0) return 0;
       return align256((size_t)block_loss_blocks(T * O) * sizeof(double));
+    case FAAR_OP_LAYERNORM_BWD:             // O = D (row length), T rows
+      if (T <= 0 || O % 8 != 0 || O > kLayerNormMaxD) return 0;
+      return align256((size_t)layernorm_partial_rows(T, O) * 2 * O * sizeof(float));
     case FAAR_OP_QUANT_RTN_BATCH:   // whatever the number and sizes of the tensors: launches reuse it in stream order
       return align256((size_t)kBatchPartials * sizeof(float));
     case FAAR_OP_INIT_V:
@@ -886,6 +890,34 @@ int faar_rmsnorm_bwd(const void* dh1, const void* dh2, const void* dh3, const vo
                                        static_cast<hipStream_t>(stream)));
 }
 
+int faar_layernorm_fwd(const void* x, faar_dtype xdt, int64_t T, int64_t D, const float* g, const float* b, float eps, void* h, float* mean,
+                       float* rstd, void* stream) {
+  if (!x || !g || !h || !mean || !rstd) return FAAR_E_NULL;
+  if (int e = check_wdt(xdt)) return e;
+  if (int e = check_rows(T, D)) return e;
+  if (D > kLayerNormMaxD) return FAAR_E_SHAPE;
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return FAAR_E_ARG;
+  if (!aligned16(x) || !aligned16(g) || !aligned16(b) || !aligned16(h)) return FAAR_E_ARG;
+  return hip_status(launch_layernorm_fwd(x, xdt == FAAR_BF16, T, D, g, b, eps, static_cast<bf16_t*>(h), mean, rstd,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+int faar_layernorm_bwd(const void* dh1, const void* dh2, const void* dh3, const void* x, faar_dtype xdt, int64_t T, int64_t D,
+                       const float* g, const float* mean, const float* rstd, const void* d_res, void* dx, float* dg, float* db, void* ws,
+                       size_t ws_bytes, void* stream) {
+  if (!dh1 || !x || !g || !mean || !rstd || !dx) return FAAR_E_NULL;
+  if (int e = check_wdt(xdt)) return e;
+  if (int e = check_rows(T, D)) return e;
+  if (D > kLayerNormMaxD) return FAAR_E_SHAPE;
+  if (!aligned16(dh1) || !aligned16(dh2) || !aligned16(dh3) || !aligned16(x) || !aligned16(g) || !aligned16(d_res) || !aligned16(dx) ||
+      !aligned16(dg) || !aligned16(db) || !aligned16(ws))
+    return FAAR_E_ARG;
+  if ((dg || db) && (!ws || ws_bytes < faar_workspace_bytes(FAAR_OP_LAYERNORM_BWD, D, 16, T, 0))) return FAAR_E_WORKSPACE;
+  return hip_status(launch_layernorm_bwd(static_cast<const bf16_t*>(dh1), static_cast<const bf16_t*>(dh2), static_cast<const bf16_t*>(dh3), x,
+                                         xdt == FAAR_BF16, T, D, g, mean, rstd, static_cast<const bf16_t*>(d_res),
+                                         static_cast<bf16_t*>(dx), dg, db, static_cast<float*>(ws), static_cast<hipStream_t>(stream)));
+}
+
 int faar_rope(const void* x, int64_t T, int64_t H, int64_t dh, const float* cos_t, const float* sin_t, int64_t S, int32_t inverse,
               void* y, void* stream) {
   if (!x || !cos_t || !sin_t || !y) return FAAR_E_NULL;
@@ -893,6 +925,32 @@ int faar_rope(const void* x, int64_t T, int64_t H, int64_t dh, const float* cos_
   if (!aligned16(x) || !aligned16(y) || !aligned16(cos_t) || !aligned16(sin_t)) return FAAR_E_ARG;
   return hip_status(launch_rope(static_cast<const bf16_t*>(x), T, H, dh, cos_t, sin_t, S, inverse != 0, static_cast<bf16_t*>(y),
                                 static_cast<hipStream_t>(stream)));
+}
+
+int faar_rope_axes(const void* q, int64_t ldq, int64_t n_q, const void* k, int64_t ldk, int64_t n_k, int64_t T, int64_t dh, int64_t rot,
+                   const int32_t* pos, int64_t n_axes, const uint8_t* axis, const double* freq, uint32_t flags, void* yq, int64_t ldyq,
+                   void* yk, int64_t ldyk, void* stream) {
+  if (!q || !yq || !pos || !axis || !freq || (!k) != (!yk)) return FAAR_E_NULL;
+  if (!k) n_k = ldk = ldyk = 0;
+  if (T <= 0 || T > 0x7FFFFFFF || n_q <= 0 || n_q > 4096 || n_k < 0 || n_k > 4096 || (k && n_k == 0)) return FAAR_E_SHAPE;
+  if (dh <= 0 || dh % 8 != 0 || dh > 2 * kRopeMaxHalf || rot <= 0 || rot % 16 != 0 || rot > dh || n_axes <= 0 || n_axes > 256) return FAAR_E_SHAPE;
+  auto bad_rows = [&](int64_t ld, int64_t heads) { return ld < heads * dh || ld % 8 != 0 || ld > kMaxElems / T; };
+  if (bad_rows(ldq, n_q) || bad_rows(ldyq, n_q) || (k && (bad_rows(ldk, n_k) || bad_rows(ldyk, n_k)))) return FAAR_E_SHAPE;
+  if (flags & ~(uint32_t)(FAAR_ROPE_PAIRS | FAAR_ROPE_INVERSE)) return FAAR_E_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(yq) || !aligned16(yk) || (reinterpret_cast<uintptr_t>(pos) & 3u)) return FAAR_E_ARG;
+  if ((q == yq && ldq != ldyq) || (k && k == yk && ldk != ldyk)) return FAAR_E_ARG;
+  RopeAxes ax{};
+  const int half = static_cast<int>(rot / 2);
+  for (int i = 0; i < half; ++i) {
+    if (axis[i] >= n_axes || !std::isfinite(freq[i])) return FAAR_E_ARG;
+    ax.axis[i] = axis[i];
+    ax.turns[i] = freq[i] * 0.15915494309189533576888;    // 1 / (2 pi)
+  }
+  const bool rest = rot < dh && (q != yq || k != yk);
+  return hip_status(launch_rope_axes({static_cast<const bf16_t*>(q), static_cast<bf16_t*>(yq), ldq, ldyq, static_cast<int>(n_q)},
+                                     {static_cast<const bf16_t*>(k), static_cast<bf16_t*>(yk), ldk, ldyk, static_cast<int>(n_k)}, T,
+                                     static_cast<int>(dh), half, pos, ax, (flags & FAAR_ROPE_INVERSE) != 0, (flags & FAAR_ROPE_PAIRS) != 0,
+                                     rest, static_cast<hipStream_t>(stream)));
 }
 
 static int check_attention(int64_t n_seq, int64_t S, int64_t n_q, int64_t n_kv, int64_t dh, float scale) {

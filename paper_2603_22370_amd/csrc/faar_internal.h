@@ -176,6 +176,19 @@ hipError_t launch_block_output_loss(const void* X, bool x_bf16, const bf16_t* Dm
 // Y (may be X) = every head of X [T, H * dh] rotated by the angles of the tables' row t % S (cos_t, sin_t [S, dh / 2])
 hipError_t launch_rope(const bf16_t* X, int64_t T, int64_t H, int64_t dh, const float* cos_t, const float* sin_t, int64_t S,
                        bool inverse, bf16_t* Y, hipStream_t st);
+// mean, rstd [T]; dg, db nullable (both null: partials unused); partials [layernorm_partial_rows][2][D]
+int64_t layernorm_partial_rows(int64_t T, int64_t D);
+hipError_t launch_layernorm_fwd(const void* X, bool x_bf16, int64_t T, int64_t D, const float* g, const float* b, float eps, bf16_t* H,
+                                float* mean, float* rstd, hipStream_t st);
+hipError_t launch_layernorm_bwd(const bf16_t* dH1, const bf16_t* dH2, const bf16_t* dH3, const void* X, bool x_bf16, int64_t T, int64_t D,
+                                const float* g, const float* mean, const float* rstd, const bf16_t* d_res, bf16_t* dX, float* dg,
+                                float* db, float* partials, hipStream_t st);
+// one of the tensors that faar_rope_axes rotates; heads 0: absent
+struct RopeTensor { const bf16_t* x; bf16_t* y; int64_t ldx, ldy; int heads; };
+constexpr int kRopeMaxHalf = 128;       // frequencies of a head
+struct RopeAxes { double turns[kRopeMaxHalf]; uint8_t axis[kRopeMaxHalf]; };   // turns per position and position axis of each frequency
+hipError_t launch_rope_axes(const RopeTensor& q, const RopeTensor& k, int64_t T, int dh, int half, const int32_t* pos, const RopeAxes& ax,
+                            bool inverse, bool pairs, bool copy_rest, hipStream_t st);
 // lse [n_q, T]
 hipError_t launch_attention_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, int64_t n_seq, int64_t S, int64_t n_q,
                                 int64_t n_kv, int64_t dh, float scale, bf16_t* O, float* lse, hipStream_t st);
