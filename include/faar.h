@@ -663,6 +663,64 @@ int faar_rope_axes(const void* q, int64_t ldq, int64_t n_q, const void* k, int64
                    const int32_t* pos, int64_t n_axes, const uint8_t* axis, const double* freq, uint32_t flags, void* yq, int64_t ldyq,
                    void* yk, int64_t ldyk, void* stream);
 
+/*
+ * Softmax attention over ragged sequences under masks, with capped or biased scores.  Sequence b is q_len[b] rows of q from row
+ * q_start[b] on and k_len[b] rows of k and v from row k_start[b] on; its queries are the LAST positions: query i stands at position
+ * p = k_len[b] - q_len[b] + i, key j at position j.  Rows may lie packed (start = sum of the lengths before), padded or in a cache
+ * (start = b * capacity); rows of no sequence are neither read nor written.  For head h and its key / value head h / (n_q / n_kv):
+ *
+ *   z = scale q.k;   s = cap tanh(z / cap) - slopes[h] |p - j|   (cap 0: s = z - ...; slopes NULL: no bias)
+ *   p sees j iff  |p - j| < window (where window > 0)  and, with FAAR_ATTENTION_CAUSAL, j <= p or j < prefix[b]
+ *   P = softmax of s over the keys that p sees;  o = P v;  lse = log of the sum of exp(s).  Sees none: o = 0, lse = -inf, no gradient.
+ *
+ * Lengths live on the device and are read there.  A plan is made from them once for a batch (once a token where tokens are generated)
+ * and read by the calls of every layer with the same description of rows, heads and mask.  On the device every call looks whether the
+ * plan is of its description; if not, or if the plan met a sequence that reaches outside 0 .. Tq / Tk, a negative prefix, or more
+ * query rows in all than there are, the call's outputs are NaN throughout.  Key rows may belong to several sequences in the forward
+ * (a shared prompt); in the backward no row may (NaN, where the lengths add up to more rows than there are; else undefined).
+ *
+ * One token a sequence (answering): q_start and q_len NULL.  Query row b is then the last position of sequence b, Tq = n_seq, and the
+ * forward splits the caches into pieces that it joins at the end.  There is no backward of this form.
+ */
+enum { FAAR_ATTENTION_CAUSAL = 1 };
+typedef struct {
+  int64_t n_seq;           /* sequences, at most 2^20 */
+  int64_t Tq, Tk;          /* rows of q, o and of k, v: at most 2^30 */
+  const int32_t* q_start;  /* in  device int32[n_seq]; q_start and q_len both NULL: one token a sequence */
+  const int32_t* q_len;
+  const int32_t* k_start;  /* in  device int32[n_seq]; k_start and k_len both NULL: those of q (and Tk = Tq) */
+  const int32_t* k_len;
+  const int32_t* prefix;   /* in  device int32[n_seq], nullable */
+  int64_t window;          /* 0: none */
+  uint32_t flags;          /* FAAR_ATTENTION_CAUSAL */
+  int64_t n_q, n_kv, dh;   /* n_q % n_kv == 0; dh a multiple of 8, at most 128 */
+  int64_t ldq, ldk, ldv, ldo; /* elements between rows of q (and dq), k (dk), v (dv), o (d_o): multiples of 8, heads side by side in a
+                                 row; q, k and v may be parts of one buffer, and so may their gradients */
+  float scale;             /* > 0 */
+  float cap;               /* 0: none */
+  const float* slopes;     /* in  device float[n_q], nullable: finite */
+} faar_attention;
+
+/* Bytes of a plan, and of the workspace of a forward (backward 0; lse wanted or not) or backward call; 0 if the description is invalid
+ * (its row strides do not matter for the plan).  Pure host functions. */
+size_t faar_attention_plan_bytes(const faar_attention* a);
+size_t faar_attention_masked_workspace_bytes(const faar_attention* a, int32_t backward);
+
+/* a: HOST pointer, read during the call.  plan: out, 16-byte aligned; good for every call with the same n_seq, Tq, Tk, window, flags,
+ * n_q, n_kv and the same form until the lengths it was made from change. */
+int faar_attention_plan(const faar_attention* a, void* plan, size_t plan_bytes, void* stream);
+
+/* q in bf16 [Tq] rows of n_q * dh, k, v in bf16 [Tk] rows of n_kv * dh, o out bf16; lse out, nullable float [n_q * Tq] (kept for the
+ * backward).  float32 arithmetic; probabilities are rounded to bf16 as matrix-core operands. */
+int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* q, const void* k, const void* v, void* o,
+                              float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* (dq, dk, dv) for the output gradient d_o; o and lse from the forward call.  dk and dv are summed over the query heads of a group in
+ * a fixed order.  Outputs must not overlap inputs. */
+int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* d_o, const void* q, const void* k,
+                              const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                              void* stream);
+
 /* a = SiLU(p) q = p sigmoid(p) q, all bf16 [n], n % 8 == 0 */
 int faar_silu_mul_fwd(const void* p, const void* q, int64_t n, void* a, void* stream);
 

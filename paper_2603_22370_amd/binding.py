@@ -53,6 +53,13 @@ class faar_block(ctypes.Structure):
                 ("lin", faar_block_linear * 7)]
 
 
+class faar_attention(ctypes.Structure):
+    _fields_ = [("n_seq", c_int64), ("Tq", c_int64), ("Tk", c_int64), ("q_start", c_void_p), ("q_len", c_void_p), ("k_start", c_void_p),
+                ("k_len", c_void_p), ("prefix", c_void_p), ("window", c_int64), ("flags", c_uint32), ("n_q", c_int64), ("n_kv", c_int64),
+                ("dh", c_int64), ("ldq", c_int64), ("ldk", c_int64), ("ldv", c_int64), ("ldo", c_int64), ("scale", c_float), ("cap", c_float),
+                ("slopes", c_void_p)]
+
+
 _lib = None
 
 
@@ -150,6 +157,18 @@ def lib() -> ctypes.CDLL:
         L.faar_layernorm_bwd.restype = c_int
         L.faar_layernorm_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
                                          c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        A = ctypes.POINTER(faar_attention)
+        L.faar_attention_plan_bytes.restype = c_size_t
+        L.faar_attention_plan_bytes.argtypes = [A]
+        L.faar_attention_masked_workspace_bytes.restype = c_size_t
+        L.faar_attention_masked_workspace_bytes.argtypes = [A, c_int32]
+        L.faar_attention_plan.restype = c_int
+        L.faar_attention_plan.argtypes = [A, c_void_p, c_size_t, c_void_p]
+        L.faar_attention_masked_fwd.restype = c_int
+        L.faar_attention_masked_fwd.argtypes = [A, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.faar_attention_masked_bwd.restype = c_int
+        L.faar_attention_masked_bwd.argtypes = [A, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                                c_void_p, c_void_p, c_size_t, c_void_p]
         L.faar_rope_axes.restype = c_int
         L.faar_rope_axes.argtypes = [c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int64, c_int64, c_void_p, c_int64,
                                      c_void_p, c_void_p, c_uint32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
@@ -209,6 +228,11 @@ def _rows(where, **ts):
 def _ld(t):
     """Elements between the starts of neighbouring rows (0: absent)."""
     return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _zeros_like_rows(t):
+    """Zeros with the shape and the row stride of t."""
+    return torch.zeros((t.shape[0], _ld(t)), dtype=t.dtype, device=t.device)[:, :t.shape[1]]
 
 
 def _check(rc: int, where: str):
@@ -649,6 +673,94 @@ def faar_attention_bwd(d_o, q, k, v, o, lse, n_seq, n_q, n_kv, scale=None, ws=No
     ws = _workspace(OP_ATTENTION_BWD, n_q * dh, n_kv * dh, T, device=q.device) if ws is None else ws
     _check(lib().faar_attention_bwd(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), n_seq, S, n_q, n_kv, dh, float(scale),
                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()), "faar_attention_bwd")
+    return dq, dk, dv
+
+
+FAAR_ATTENTION_CAUSAL = 1
+
+
+def attention_description(n_q, n_kv, dh, Tq, Tk, start, length, k_start=None, k_len=None, single=False, prefix=None, window=0, causal=True,
+                          scale=None, cap=0.0, slopes=None):
+    """A faar_attention for the calls below (see faar.h).  start, length: int32 device tensors [n_seq], the rows of each sequence in q, and
+    in k and v where k_start, k_len do not say otherwise; single: one token a sequence, start and length are those of the caches.
+    Keeps references to every tensor it points to."""
+    if single and k_start is not None:
+        raise ValueError("attention_description: the sequences of single tokens are those of the caches")
+    q = (None, None) if single else (start, length)
+    k = (start, length) if single else (k_start, k_len)
+    _dev(*q, *k, prefix, slopes)
+    n_seq = length.numel()
+    if any(t is not None and (t.dtype != torch.int32 or t.numel() != n_seq) for t in (*q, *k, prefix)):
+        raise ValueError("attention_description: starts, lengths and prefixes are int32 [n_seq]")
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.numel() != n_q):
+        raise ValueError("attention_description: slopes float32 [n_q]")
+    a = faar_attention()
+    a.n_seq, a.Tq, a.Tk, a.window, a.flags = n_seq, Tq, Tk, window, FAAR_ATTENTION_CAUSAL if causal else 0
+    a.q_start, a.q_len, a.k_start, a.k_len, a.prefix, a.slopes = (_ptr(t) for t in (*q, *k, prefix, slopes))
+    a.n_q, a.n_kv, a.dh = n_q, n_kv, dh
+    a.ldq = a.ldo = n_q * dh
+    a.ldk = a.ldv = n_kv * dh
+    a.scale, a.cap = dh ** -0.5 if scale is None else float(scale), float(cap)
+    a._keep = [*q, *k, prefix, slopes]
+    a._device = length.device
+    return a
+
+
+def faar_attention_plan(a, out=None):
+    """The plan of a description's masks, read by the calls of every layer -> uint8 device tensor."""
+    _dev(out)
+    n = int(lib().faar_attention_plan_bytes(ctypes.byref(a)))
+    plan = torch.empty(n, dtype=torch.uint8, device=a._device) if out is None else out
+    _check(lib().faar_attention_plan(ctypes.byref(a), _ptr(plan), plan.numel(), _stream()), "faar_attention_plan")
+    return plan
+
+
+def attention_masked_workspace(a, backward=False):
+    """A workspace for the forward, and with backward for both."""
+    n = max(int(lib().faar_attention_masked_workspace_bytes(ctypes.byref(a), b)) for b in ((0, 1) if backward else (0,)))
+    if n == 0:
+        raise FaarError(-2, "faar_attention_masked_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=a._device)
+
+
+def _masked_rows(a, where, q, k, v, o, lse=None):
+    _rows(where, q=q, k=k, v=v, o=o)
+    _dev(lse)
+    kv = (a.Tk, a.n_kv * a.dh)
+    if q.shape != (a.Tq, a.n_q * a.dh) or o.shape != q.shape or k.shape != kv or v.shape != kv or \
+            (lse is not None and (lse.dtype != torch.float32 or lse.numel() != a.n_q * a.Tq)):
+        raise ValueError(f"{where}: q, o [Tq, n_q * dh]; k, v [Tk, n_kv * dh]; lse float32 [n_q, Tq]")
+    d = faar_attention.from_buffer_copy(a)               # the caller's description may be in use by another thread
+    d.ldq, d.ldk, d.ldv, d.ldo = _ld(q), _ld(k), _ld(v), _ld(o)
+    return d
+
+
+def faar_attention_masked_fwd(a, plan, q, k, v, out=None, want_lse=True, ws=None):
+    """-> (o bf16 [Tq, n_q * dh], lse float32 [n_q, Tq] or None).  Rows of no sequence keep what out holds (0 where out is not given)."""
+    o = torch.zeros((a.Tq, a.n_q * a.dh), dtype=torch.bfloat16, device=q.device) if out is None else out
+    lse = torch.empty((a.n_q, a.Tq), dtype=torch.float32, device=q.device) if want_lse else None
+    d = _masked_rows(a, "faar_attention_masked_fwd", q, k, v, o)
+    ws = attention_masked_workspace(a) if ws is None else ws
+    _dev(plan, ws)
+    _check(lib().faar_attention_masked_fwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(ws),
+                                           ws.numel(), _stream()), "faar_attention_masked_fwd")
+    return o, lse
+
+
+def faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, lse, out=None, ws=None):
+    """-> (dq, dk, dv) bf16, shaped like q, k, v (out: the same three, with the row strides of q, k and v).  Rows of no sequence keep what
+    out holds (0 where out is not given)."""
+    if out is None:
+        out = tuple(_zeros_like_rows(t) for t in (q, k, v))
+    dq, dk, dv = out
+    d = _masked_rows(a, "faar_attention_masked_bwd", q, k, v, o, lse)
+    _rows("faar_attention_masked_bwd", d_o=d_o, dq=dq, dk=dk, dv=dv)
+    if any(x.shape != y.shape or _ld(x) != _ld(y) for x, y in ((d_o, o), (dq, q), (dk, k), (dv, v))):
+        raise ValueError("faar_attention_masked_bwd: gradients have the shapes and row strides of what they belong to")
+    ws = attention_masked_workspace(a, backward=True) if ws is None else ws
+    _dev(plan, ws)
+    _check(lib().faar_attention_masked_bwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
+                                           _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()), "faar_attention_masked_bwd")
     return dq, dk, dv
 
 

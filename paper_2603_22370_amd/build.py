@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libfaar.so")
 SOURCES = ["faar_api.hip", "faar_elementwise.hip", "faar_gemm.hip", "faar_small.hip", "faar_stage2.hip", "faar_block.hip", "faar_attention.hip",
-           "faar_layernorm.hip", "faar_rope_axes.hip"]
+           "faar_layernorm.hip", "faar_rope_axes.hip", "faar_masked_attention.hip"]
 
 # -ffp-contract=off: the decision arithmetic must round once per operation (bit-exact parity).
 # packed-fp32 ops are off: some of their forms have given wrong results on this hardware.

@@ -990,6 +990,114 @@ int faar_attention_bwd(const void* d_o, const void* q, const void* k, const void
                                          static_cast<bf16_t*>(dv), st));
 }
 
+// ---- attention under masks ---------------------------------------------------------------------------------------------
+namespace {
+
+struct MaskedCall {
+  PlanTag tag;
+  PlanSizes z;
+  MaskedDims d;
+  bool single;
+};
+
+int masked_call(const faar_attention* a, MaskedCall& c) {
+  if (!a) return FAAR_E_NULL;
+  c.single = !a->q_start && !a->q_len;
+  if ((!a->q_start) != (!a->q_len) || (!a->k_start) != (!a->k_len) || (c.single && !a->k_start)) return FAAR_E_NULL;
+  constexpr int64_t kMaxRows = (int64_t)1 << 30;
+  if (a->n_seq <= 0 || a->n_seq > ((int64_t)1 << 20) || a->Tq <= 0 || a->Tk <= 0 || a->Tq > kMaxRows || a->Tk > kMaxRows) return FAAR_E_SHAPE;
+  if ((c.single && a->Tq != a->n_seq) || (!a->k_start && a->Tk != a->Tq)) return FAAR_E_SHAPE;
+  if (a->n_q <= 0 || a->n_kv <= 0 || a->n_q % a->n_kv != 0 || a->n_q > 4096 || a->dh <= 0 || a->dh % 8 != 0 || a->dh > 128) return FAAR_E_SHAPE;
+  if (a->window < 0 || (a->flags & ~(uint32_t)FAAR_ATTENTION_CAUSAL)) return FAAR_E_ARG;
+  if (!(a->scale > 0.0f) || !std::isfinite(a->scale) || !(a->cap >= 0.0f) || !std::isfinite(a->cap)) return FAAR_E_ARG;
+  for (const int32_t* p : {a->q_start, a->q_len, a->k_start, a->k_len, a->prefix})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return FAAR_E_ARG;
+  if (reinterpret_cast<uintptr_t>(a->slopes) & 3u) return FAAR_E_ARG;
+  c.z = attention_plan_sizes(a->n_seq, a->Tq, a->Tk, a->n_q, a->n_kv, c.single);
+  // the largest grids: work items x heads, and for single tokens one query head of a sequence each
+  if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * a->n_kv > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
+  const int window = a->window > kMaxRows ? 0 : static_cast<int>(a->window);     // wider than any sequence: none
+  const int tag[kPlanTagWords] = {0x5A11FAA3, static_cast<int>(a->flags) | (c.single ? 2 : 0), static_cast<int>(a->n_seq), static_cast<int>(a->Tq),
+                                  static_cast<int>(a->Tk), window, static_cast<int>(a->n_q), static_cast<int>(a->n_kv)};
+  for (int i = 0; i < kPlanTagWords; ++i) c.tag.w[i] = tag[i];
+  constexpr float kL2e = 1.4426950408889634f;
+  const float cap_a = a->cap * kL2e, cap_b = a->cap > 0.0f ? 2.0f * kL2e * a->scale / a->cap : 0.0f;
+  if (!std::isfinite(cap_a) || !std::isfinite(cap_b) || !std::isfinite(a->scale * kL2e)) return FAAR_E_ARG;
+  c.d = MaskedDims{static_cast<int>(a->n_q), static_cast<int>(a->n_kv), static_cast<int>(a->dh), a->Tq, a->Tk, a->ldq, a->ldk, a->ldv, a->ldo,
+                   a->scale, a->scale * kL2e, cap_a, cap_b, std::min(cap_a, 110.0f - cap_a), a->slopes};
+  return FAAR_OK;
+}
+
+int masked_rows(const faar_attention* a) {
+  const int64_t wide = (int64_t)1 << 24;               // a tile's offsets are 32-bit
+  const int64_t q = a->n_q * a->dh, k = a->n_kv * a->dh;
+  for (int64_t ld : {a->ldq, a->ldk, a->ldv, a->ldo})
+    if (ld % 8 != 0 || ld > wide) return FAAR_E_SHAPE;
+  return a->ldq < q || a->ldo < q || a->ldk < k || a->ldv < k ? FAAR_E_SHAPE : FAAR_OK;
+}
+
+size_t masked_ws_bytes(const MaskedCall& c, bool backward) {
+  if (backward) return align256((size_t)c.d.n_q * c.d.Tq * sizeof(float));        // rowsum(dO o) per head and query
+  if (c.single) return align256((size_t)c.z.max_q * c.d.n_q * (c.d.dh + 2) * sizeof(float));
+  return 256;                                          // none needed
+}
+
+}  // namespace
+
+size_t faar_attention_plan_bytes(const faar_attention* a) {
+  MaskedCall c;
+  return masked_call(a, c) == FAAR_OK ? align256((size_t)c.z.words * 4) : 0;
+}
+
+size_t faar_attention_masked_workspace_bytes(const faar_attention* a, int32_t backward) {
+  MaskedCall c;
+  if (masked_call(a, c) != FAAR_OK || (backward && c.single)) return 0;
+  return masked_ws_bytes(c, backward != 0);
+}
+
+int faar_attention_plan(const faar_attention* a, void* plan, size_t plan_bytes, void* stream) {
+  if (!a || !plan) return FAAR_E_NULL;
+  MaskedCall c;
+  if (int e = masked_call(a, c)) return e;
+  if (!aligned16(plan)) return FAAR_E_ARG;
+  if (plan_bytes < align256((size_t)c.z.words * 4)) return FAAR_E_WORKSPACE;
+  return hip_status(launch_attention_plan(a->q_start, a->q_len, a->k_start ? a->k_start : a->q_start, a->k_len ? a->k_len : a->q_len, a->prefix,
+                                          c.tag, c.z, static_cast<int*>(plan), static_cast<hipStream_t>(stream)));
+}
+
+int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* q, const void* k, const void* v, void* o,
+                              float* lse, void* ws, size_t ws_bytes, void* stream) {
+  if (!a || !plan || !q || !k || !v || !o) return FAAR_E_NULL;
+  MaskedCall c;
+  if (int e = masked_call(a, c)) return e;
+  if (int e = masked_rows(a)) return e;
+  if (!aligned16(plan) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(ws) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return FAAR_E_ARG;
+  if (plan_bytes < align256((size_t)c.z.words * 4) || !ws || ws_bytes < masked_ws_bytes(c, false)) return FAAR_E_WORKSPACE;
+  return hip_status(launch_masked_fwd(static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v),
+                                      static_cast<const int*>(plan), c.tag, c.z, c.d, c.single, static_cast<bf16_t*>(o), lse,
+                                      static_cast<float*>(ws), static_cast<hipStream_t>(stream)));
+}
+
+int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* d_o, const void* q, const void* k,
+                              const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                              void* stream) {
+  if (!a || !plan || !d_o || !q || !k || !v || !o || !lse || !dq || !dk || !dv) return FAAR_E_NULL;
+  MaskedCall c;
+  if (int e = masked_call(a, c)) return e;
+  if (c.single) return FAAR_E_UNSUPPORTED;
+  if (int e = masked_rows(a)) return e;
+  for (const void* p : {plan, d_o, q, k, v, o, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(ws)})
+    if (!aligned16(p)) return FAAR_E_ARG;
+  if (reinterpret_cast<uintptr_t>(lse) & 3u) return FAAR_E_ARG;
+  if (plan_bytes < align256((size_t)c.z.words * 4) || !ws || ws_bytes < masked_ws_bytes(c, true)) return FAAR_E_WORKSPACE;
+  return hip_status(launch_masked_bwd(static_cast<const bf16_t*>(d_o), static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k),
+                                      static_cast<const bf16_t*>(v), static_cast<const bf16_t*>(o), lse, static_cast<const int*>(plan), c.tag, c.z,
+                                      c.d, static_cast<float*>(ws), static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk), static_cast<bf16_t*>(dv),
+                                      static_cast<hipStream_t>(stream)));
+}
+
 int faar_silu_mul_fwd(const void* p, const void* q, int64_t n, void* a, void* stream) {
   if (!p || !q || !a) return FAAR_E_NULL;
   if (n <= 0 || n % 8 != 0 || n > kMaxElems) return FAAR_E_SHAPE;

@@ -189,6 +189,28 @@ constexpr int kRopeMaxHalf = 128;       // frequencies of a head
 struct RopeAxes { double turns[kRopeMaxHalf]; uint8_t axis[kRopeMaxHalf]; };   // turns per position and position axis of each frequency
 hipError_t launch_rope_axes(const RopeTensor& q, const RopeTensor& k, int64_t T, int dh, int half, const int32_t* pos, const RopeAxes& ax,
                             bool inverse, bool pairs, bool copy_rest, hipStream_t st);
+// Attention under masks.  The plan is an array of ints: a tag (what it was made for), its counts, then the work items, 8 words each.
+enum { kTagMagic = 0, kTagFlags, kTagSeqs, kTagTq, kTagTk, kTagWindow, kTagNq, kTagNkv, kPlanTagWords };   // flags: 1 causal, 2 single tokens
+enum { kPlanBad = kPlanTagWords, kPlanNoBackward, kPlanQItems, kPlanKItems };
+constexpr int kPieceKeys = 128;         // single tokens: keys of a block
+struct PlanTag { int w[kPlanTagWords]; };
+struct PlanSizes { int q_at, k_at, seq_at, target; int64_t max_q, max_k, words; };   // places (words), bounds of the item counts
+struct MaskedDims {
+  int n_q, n_kv, dh;
+  int64_t Tq, Tk, ldq, ldk, ldv, ldo;   // rows; elements between rows
+  float scale, c, cap_a, cap_b, ref;    // c = scale log2 e; cap_a = cap log2 e (0: none), cap_b = 2 scale log2 e / cap; ref: see launch_masked_fwd
+  const float* slopes;                  // nullable [n_q]
+};
+PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, bool single);
+hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int* k_start, const int* k_len, const int* prefix, const PlanTag& tag,
+                                 const PlanSizes& z, int* plan, hipStream_t st);
+// part (single tokens): [max_q][n_q][dh + 2]
+hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
+                             const MaskedDims& d, bool single, bf16_t* O, float* lse, float* part, hipStream_t st);
+// delta: [n_q][Tq]
+hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const float* lse,
+                             const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
+                             bf16_t* dV, hipStream_t st);
 // lse [n_q, T]
 hipError_t launch_attention_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, int64_t n_seq, int64_t S, int64_t n_q,
                                 int64_t n_kv, int64_t dh, float scale, bf16_t* O, float* lse, hipStream_t st);

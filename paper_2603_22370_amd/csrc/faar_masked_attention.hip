@@ -1,0 +1,931 @@
+// Attention between the q / k / v and the output projections of blocks whose scores are capped by a tanh or carry a bias that falls
+// with the distance, under document, prefix, window and whole-sequence masks; forward and backward over ragged sequences, and the
+// forward for one token a sequence over a cache.  For a query at position p of its sequence and a key at position j, both of one
+// head and key / value head,
+//   z = scale q.k,  s = cap tanh(z / cap) - slope |p - j|  (no cap: z),  P = softmax of s over the keys that p sees,  o = P v
+//   dv = P^T dO,  ds = P (dO v^T - rowsum(dO o)),  dz = ds (1 - tanh^2),  dq = scale dz k,  dk = scale dz^T q.
+//
+// Masks.  With the queries as the last positions of their sequence, what the masks leave of a query's keys is an interval
+// [lo(p), hi(p)) whose ends grow with p, and so are the queries that see a key.  A block of 64 keys is then skipped, taken whole, or
+// compared element by element (one subtraction, one comparison), and blocks outside a tile's interval are never loaded.
+//
+// Plan.  Sequence lengths live on the device.  A plan, made by one small launch for a batch and read by every layer, lists the work
+// items: tiles of 128 queries (forward, dq) and of 64 keys (dk, dv) that each lie inside one sequence, the most expensive first, or
+// for single tokens the pieces of the caches.  A workgroup reads its item with one scalar load; the grid is the largest number of
+// items that any lengths can give, and workgroups behind the last item end at once.
+//
+// Tiles, copies and products are those of the causal kernels (faar_attention.hip): 64-token tiles in LDS by asynchronous copies, two
+// stages, 32 queries (keys) a wavefront, v_mfma_f32_32x32x16_bf16, probabilities in the accumulator layout as the next operand.
+// P and dz are rounded to bf16 as matrix-core operands, like there: half the cost of the products' time is what exact ones would add
+// in a second product each, and the outputs are bf16.  Everything else is float32.
+#include <algorithm>
+
+#include "faar_attention_tile.h"
+
+namespace faar {
+namespace {
+
+constexpr float kLowest = -1.7e38f;    // "no score yet": below every score, and finite, so that differences stay numbers
+constexpr float kLazy = 8.0f;          // the reference maximum is raised when a score exceeds it by more than 2^kLazy
+
+// how scores become exponents: as they are; with a bias; capped with every exponent in range of a fixed reference; capped with a
+// running maximum (and a bias)
+enum { kPlain = 0, kBiased = 1, kBounded = 2, kCapped = 3 };
+
+__device__ __attribute__((aligned(16))) const uint32_t kZeroChunk[4] = {0, 0, 0, 0};
+
+// 16 bytes per lane from that lane's own address
+__device__ __forceinline__ void dma16_from(const void* gptr, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory", "m0");
+}
+// 64 rows of a tile of which `valid` are there and dh of its columns: whole tiles by the copies that need no comparison; what is
+// missing is filled with zeros (a masked probability of 0 times whatever lies behind a sequence would not be 0 for all values)
+template <int DH>
+__device__ __forceinline__ void copy_tile(const bf16_t* __restrict__ src, int64_t row0, int valid, int64_t ld, int64_t col0, int dh,
+                                          uint32_t lane_offset, uint32_t tile, int wave, int tid) {
+  typedef Tile<DH> Tl;
+  if (valid >= kTok && dh == DH) {
+    // addresses that are the same for all lanes go in scalar registers, said lane by lane where the compiler does not see it
+#pragma unroll
+    for (int j = 0; j < Tl::COPIES; ++j) {
+      const uint64_t at = reinterpret_cast<uint64_t>(src + (row0 + j * (256 / Tl::CPR)) * ld + col0);
+      const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+      dma16(reinterpret_cast<const void*>(static_cast<uint64_t>(hi) << 32 | lo), lane_offset, __builtin_amdgcn_readfirstlane(tile + 4096u * j + 1024u * wave));
+    }
+    return;
+  }
+  asm volatile("" : "+v"(tid));        // addresses are formed here, where few blocks come by, and not kept in registers throughout
+  const int r = tid / Tl::CPR, col = ((tid % Tl::CPR) ^ Tl::key(r)) * 8;
+#pragma unroll
+  for (int j = 0; j < Tl::COPIES; ++j) {
+    const int row = r + j * (256 / Tl::CPR);
+    const void* p = row < valid && col < dh ? static_cast<const void*>(src + (row0 + row) * ld + col0 + col) : kZeroChunk;
+    dma16_from(p, __builtin_amdgcn_readfirstlane(tile + 4096u * j + 1024u * wave));
+  }
+}
+
+struct Seen { int lo, hi; };           // keys [lo, hi) of the sequence; hi <= lo: none
+__device__ __forceinline__ Seen keys_of(int p, int k_len, int prefix, int window, bool causal) {
+  int lo = 0, hi = causal ? max(p + 1, prefix) : k_len;
+  if (window > 0) {
+    lo = max(lo, p - window + 1);
+    hi = min(hi, p + window);
+  }
+  return {lo, min(hi, k_len)};
+}
+// queries [lo, hi) of the sequence (by index, query i at position i + off) that see key j
+__device__ __forceinline__ Seen queries_of(int j, int q_len, int off, int prefix, int window, bool causal) {
+  int lo = 0, hi = q_len;
+  if (causal && j >= prefix) lo = max(lo, j - off);
+  if (window > 0) {
+    lo = max(lo, j - window + 1 - off);
+    hi = min(hi, j + window - off);
+  }
+  return {lo, hi};
+}
+
+// ---- the plan -----------------------------------------------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024, kBuckets = 128;
+
+__device__ __forceinline__ bool inside(int start, int len, int T) { return start >= 0 && len >= 0 && start <= T && len <= T - start; }
+
+__global__ void __launch_bounds__(kPlanThreads)
+k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len, const int* __restrict__ k_start, const int* __restrict__ k_len,
+                 const int* __restrict__ prefix, PlanTag tag, PlanSizes z, int* __restrict__ plan) {
+  const int n_seq = tag.w[kTagSeqs], Tq = tag.w[kTagTq], Tk = tag.w[kTagTk], window = tag.w[kTagWindow];
+  const bool causal = tag.w[kTagFlags] & 1, single = tag.w[kTagFlags] & 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ unsigned long long sums[2];              // rows of q, of k
+  __shared__ int most[2], bad, hist[2][kBuckets], scan[kPlanThreads], carry;
+  if (tid < 2) {
+    sums[tid] = 0;
+    most[tid] = 0;
+    bad = 0;
+    carry = 0;
+  }
+  for (int i = tid; i < 2 * kBuckets; i += kPlanThreads) hist[i / kBuckets][i % kBuckets] = 0;
+  __syncthreads();
+  auto blocks_of = [&](int b) {                       // single tokens: blocks of kPieceKeys keys that sequence b's token sees
+    const int n = k_len[b];
+    if (!inside(k_start[b], n, Tk)) return 0;
+    const int seen = window > 0 ? min(n, window) : n;
+    return (seen + kPieceKeys - 1) / kPieceKeys;
+  };
+  for (int b = tid; b < n_seq; b += kPlanThreads) {
+    const int kl = k_len[b], ql = single ? 1 : q_len[b];
+    if (!inside(k_start[b], kl, Tk) || (!single && !inside(q_start[b], ql, Tq)) || (prefix && prefix[b] < 0)) {
+      bad = 1;
+      continue;
+    }
+    atomicAdd(&sums[0], static_cast<unsigned long long>(single ? blocks_of(b) : ql));
+    atomicAdd(&sums[1], static_cast<unsigned long long>(kl));
+    atomicMax(&most[0], (kl + kTok - 1) / kTok);
+    atomicMax(&most[1], (ql + kTok - 1) / kTok);
+  }
+  __syncthreads();
+  // overlapping sequences would need more items than there is room for
+  const bool refuse = bad || (!single && sums[0] > static_cast<unsigned long long>(Tq));
+  const bool keys_once = !refuse && !single && sums[1] <= static_cast<unsigned long long>(Tk);   // else no backward
+  if (tid < kPlanTagWords) plan[tid] = tag.w[tid];
+  if (tid == 0) {
+    plan[kPlanBad] = refuse;
+    plan[kPlanNoBackward] = !keys_once;
+  }
+  if (refuse) return;
+
+  if (single) {
+    // pieces of whole blocks, as equal as the total over the sequences allows; every sequence has one at least
+    const int per = static_cast<int>(max(1ull, (sums[0] + z.target - 1) / z.target));
+    for (int b0 = 0; b0 < n_seq; b0 += kPlanThreads) {
+      const int b = b0 + tid;
+      const int blocks = b < n_seq ? blocks_of(b) : 0, n = b < n_seq ? max(1, (blocks + per - 1) / per) : 0;
+      scan[tid] = n;
+      __syncthreads();
+      for (int d = 1; d < kPlanThreads; d *= 2) {
+        const int v = tid >= d ? scan[tid - d] : 0;
+        __syncthreads();
+        scan[tid] += v;
+        __syncthreads();
+      }
+      const int first = carry + scan[tid] - n;
+      if (b < n_seq) {
+        const int kl = k_len[b], lo = window > 0 ? max(0, kl - window) : 0;
+        plan[z.seq_at + 2 * b] = first;
+        plan[z.seq_at + 2 * b + 1] = n;
+        for (int i = 0; i < n; ++i) {
+          const int j0 = min(kl, lo + i * per * kPieceKeys), j1 = min(kl, j0 + per * kPieceKeys);
+          int* w = plan + z.q_at + 8 * (first + i);
+          w[0] = b;
+          w[1] = k_start[b] + j0;
+          w[2] = j1 - j0;
+          w[3] = kl - 1 - j0;                          // distance of the piece's first key
+          w[4] = n;
+          w[5] = w[6] = w[7] = 0;
+        }
+      }
+      __syncthreads();
+      if (tid == kPlanThreads - 1) carry = first + n;
+      __syncthreads();
+    }
+    if (tid == 0) {
+      plan[kPlanQItems] = carry;
+      plan[kPlanKItems] = 0;
+    }
+    return;
+  }
+
+  // two passes over all items, a wavefront a sequence and a lane a tile: count the items of each cost, then place them, the most
+  // expensive first.  Items of one cost come in no particular order; no result depends on it.
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int b = wave; b < n_seq; b += kPlanThreads / 64) {
+      const int ql = q_len[b], kl = k_len[b], qs = q_start[b], ks = k_start[b], off = kl - ql;
+      const int pre = prefix ? min(prefix[b], kl) : 0;
+      for (int t = lane; t < (ql + 127) / 128; t += 64) {
+        const int r0 = 128 * t, n = min(128, ql - r0), p = off + r0;
+        const int lo = keys_of(p, kl, pre, window, causal).lo, hi = keys_of(p + n - 1, kl, pre, window, causal).hi;
+        const int b0 = hi > lo ? lo / kTok : 0, b1 = hi > lo ? (hi + kTok - 1) / kTok : 0;
+        const int bucket = kBuckets - 1 - static_cast<int>(static_cast<int64_t>(b1 - b0) * kBuckets / (most[0] + 1));
+        const int at = atomicAdd(&hist[0][bucket], 1);
+        if (pass == 1) {
+          int* w = plan + z.q_at + 8 * at;
+          w[0] = qs + r0; w[1] = n; w[2] = p; w[3] = ks; w[4] = kl; w[5] = pre; w[6] = b0; w[7] = b1;
+        }
+      }
+      if (!keys_once) continue;
+      for (int t = lane; t < (kl + kTok - 1) / kTok; t += 64) {
+        const int k0 = kTok * t, n = min(kTok, kl - k0);
+        const int lo = queries_of(k0, ql, off, pre, window, causal).lo, hi = queries_of(k0 + n - 1, ql, off, pre, window, causal).hi;
+        const int cost = hi > lo ? (hi + kTok - 1) / kTok - lo / kTok : 0;
+        const int bucket = kBuckets - 1 - static_cast<int>(static_cast<int64_t>(cost) * kBuckets / (most[1] + 1));
+        const int at = atomicAdd(&hist[1][bucket], 1);
+        if (pass == 1) {
+          int* w = plan + z.k_at + 8 * at;
+          w[0] = ks + k0; w[1] = n; w[2] = k0; w[3] = qs; w[4] = ql; w[5] = off; w[6] = pre; w[7] = 0;
+        }
+      }
+    }
+    __syncthreads();
+    if (pass == 0 && tid < 2) {                        // counts -> first place of each cost
+      int at = 0;
+      for (int i = 0; i < kBuckets; ++i) {
+        const int n = hist[tid][i];
+        hist[tid][i] = at;
+        at += n;
+      }
+      plan[tid == 0 ? kPlanQItems : kPlanKItems] = at;
+    }
+    __syncthreads();
+  }
+}
+
+// x, in a way that the compiler cannot carry over from an earlier place: what is cheap to form again does not occupy registers in between
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// a word of the plan, the same for all lanes
+__device__ __forceinline__ int word(const int* p) { return __builtin_amdgcn_readfirstlane(*p); }
+
+// Is this the plan of the call's description?  Every workgroup looks (uniform loads); what is not is answered with NaN.
+__device__ __forceinline__ bool plan_is(const int* __restrict__ plan, const PlanTag& tag, bool backward) {
+  bool ok = word(plan + kPlanBad) == 0 && !(backward && word(plan + kPlanNoBackward) != 0);
+#pragma unroll
+  for (int i = 0; i < kPlanTagWords; ++i) ok = ok && word(plan + i) == tag.w[i];
+  return ok;
+}
+__device__ __forceinline__ void fill_nan(bf16_t* p, int64_t rows, int64_t width, int64_t ld) {
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int64_t c = threadIdx.x; c < width; c += blockDim.x) p[r * ld + c] = 0x7FC0;
+}
+__device__ __forceinline__ void fill_nan(float* p, int64_t n) {
+  for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) p[i] = __uint_as_float(0x7FC00000u);
+}
+
+// ---- scores ---------------------------------------------------------------------------------------------------------------------
+struct Scores {
+  float c;             // scale log2(e): z in units of log 2
+  float a, b;          // capped: a = cap log2(e); tanh(z / cap) = 1 - 2 / (1 + 2^(b q.k))
+  float ref;           // kBounded: the fixed reference of the exponents
+  float slope;         // slope log2(e)
+};
+__device__ __forceinline__ Scores scores_of(const MaskedDims& d, int head, bool biased) {
+  return {d.c, d.cap_a, d.cap_b, d.ref, biased && d.slopes ? d.slopes[head] * kLog2e : 0.0f};
+}
+// 1 / (1 + 2^(b q.k)) = (1 - tanh) / 2
+__device__ __forceinline__ float cap_half(const Scores& sc, float x) {
+  return __builtin_amdgcn_rcpf(1.0f + fast_exp2(x * sc.b));
+}
+
+// ---- forward --------------------------------------------------------------------------------------------------------------------
+template <int DH>
+struct MaskedState {
+  bf16x8 qf[DH / 16];
+  f32x16 oacc[DH / 32];   // rows = dh, column = query lane % 32
+  float mc, l;            // reference maximum (units of log 2), and this half-wave's share of the denominator
+};
+
+// NT x 32 keys of tiles at k_lds, v_lds (first 32: half `h0`).  first: index of the lane's first key relative to what is compared:
+// `len` keys from 0 on are seen (masked); gap: distance of the lane's first key from its query.
+template <int DH, int kMode, int NT>
+__device__ __forceinline__ void masked_block(MaskedState<DH>& st, uint32_t k_lds, uint32_t v_lds, uint32_t ra, uint32_t ca, const Scores& sc,
+                                             int h0, bool masked, int first, int len, float gap) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  typedef Tile<DH> Tl;
+  f32x16 s[NT];            // rows = keys, column = query
+#pragma unroll
+  for (int kt = 0; kt < NT; ++kt) s[kt] = zero16();
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt) s[kt] = mfma(Tl::rows(k_lds + ra, h0 + kt, ks), st.qf[ks], s[kt]);
+#pragma unroll
+  for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int j = 32 * kt + 8 * (v / 4) + v % 4;     // + 4 (lane / 32), which first and gap hold
+      float x = s[kt][v];
+      if constexpr (kMode == kBounded) x = fmaf(-2.0f * sc.a, cap_half(sc, x), sc.a - sc.ref);
+      if constexpr (kMode == kCapped) x = fmaf(-2.0f * sc.a, cap_half(sc, x), sc.a);
+      if constexpr (kMode == kBiased) x = x * sc.c;
+      if constexpr (kMode == kBiased || kMode == kCapped) x = fmaf(-sc.slope, fabsf(gap - static_cast<float>(j)), x);
+      s[kt][v] = x;
+    }
+  if (masked) {
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        s[kt][v] = static_cast<uint32_t>(first + 32 * kt + 8 * (v / 4) + v % 4) < static_cast<uint32_t>(len) ? s[kt][v] : -INFINITY;
+  }
+  if constexpr (DH == 128 && (kMode == kBiased || kMode == kCapped)) __builtin_amdgcn_sched_barrier(0);   // registers
+  if constexpr (kMode != kBounded) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kt][v]);
+    mx = half_max(mx);
+    if constexpr (kMode == kPlain) mx *= sc.c;
+    if (__any(mx > st.mc + kLazy)) {
+      const float nm = fmaxf(st.mc, mx);
+      const float alpha = fast_exp2(st.mc - nm);
+      st.mc = nm;
+      st.l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) st.oacc[dt] *= alpha;
+    }
+  }
+  float ps = 0.0f;
+#pragma unroll
+  for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      float p;
+      if constexpr (kMode == kPlain) p = fast_exp2(fmaf(s[kt][v], sc.c, -st.mc));
+      else if constexpr (kMode == kBounded) p = fast_exp2(s[kt][v]);
+      else p = fast_exp2(s[kt][v] - st.mc);
+      s[kt][v] = p;
+      ps += p;
+    }
+  st.l += ps;
+#pragma unroll
+  for (int kt = 0; kt < NT; ++kt) {
+    const bf16x8 p0 = pack8<0>(s[kt]), p1 = pack8<1>(s[kt]);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 0, dt), p0, st.oacc[dt]);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 1, dt), p1, st.oacc[dt]);
+  }
+}
+
+template <int DH, int kMode>
+__global__ void __launch_bounds__(256, 2)
+k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
+             PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  typedef Tile<DH> Tl;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
+  if (!plan_is(plan, tag, false)) {
+    fill_nan(O, d.Tq, (int64_t)d.n_q * d.dh, d.ldo);
+    if (lse) fill_nan(lse, d.Tq * d.n_q);
+    return;
+  }
+  const int item = blockIdx.x / d.n_q, pair = blockIdx.x % d.n_q;
+  if (item >= word(plan + kPlanQItems)) return;
+  const int* w = plan + z.q_at + 8 * item;
+  const int row0 = word(w + 0), rows = word(w + 1), pos0 = word(w + 2), k_start = word(w + 3), k_len = word(w + 4), prefix = word(w + 5), kb0 = word(w + 6), kb1 = word(w + 7);
+  const int window = tag.w[kTagWindow];
+  const bool causal = tag.w[kTagFlags] & 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
+  const int kvh = pair % d.n_kv, head = kvh * (d.n_q / d.n_kv) + pair / d.n_kv;
+  const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped);
+
+  const int mine = min(32, rows - 32 * wave);          // this wavefront's queries (none: <= 0)
+  const bool live = n < mine;
+  const int p = pos0 + 32 * wave + n;
+  const Seen seen = live ? keys_of(p, k_len, prefix, window, causal) : Seen{0, 0};
+  const Seen sa = keys_of(pos0 + 32 * wave, k_len, prefix, window, causal), sb = keys_of(pos0 + 32 * wave + mine - 1, k_len, prefix, window, causal);
+
+  MaskedState<DH> st;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    st.qf[ks] = live && ks * 16 + 8 * hi < d.dh ? load_frag16(Q + ((int64_t)row0 + 32 * wave + n) * d.ldq + head * d.dh + ks * 16 + 8 * hi) : bf16x8{};
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = zero16();
+  st.mc = kMode == kBounded ? sc.ref : kLowest;
+  st.l = 0.0f;
+  const int64_t kvcol = (int64_t)kvh * d.dh;
+  const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
+  const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
+  auto request = [&](int kb) {
+    const uint32_t at = lds0 + (kb & 1) * (2 * Tl::ELEMS * 2);
+    copy_tile<DH>(K, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
+    copy_tile<DH>(V, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldv, kvcol, d.dh, from_v, at + Tl::ELEMS * 2, wave, tid);
+  };
+  if (kb0 < kb1) request(kb0);
+  for (int kb = kb0; kb < kb1; ++kb) {
+    FAAR_WAIT_VMCNT(0);                                // block kb has landed (mine); the barrier: everybody's, and nobody reads
+    __syncthreads();                                   // the other stage any more
+    if (kb + 1 < kb1) request(kb + 1);
+    const uint32_t k_lds = lds0 + (kb & 1) * (2 * Tl::ELEMS * 2), v_lds = k_lds + Tl::ELEMS * 2;
+    const int k0 = kb * kTok;
+    if (mine <= 0 || k0 >= sb.hi || k0 + kTok <= sa.lo) continue;
+    const float gap = static_cast<float>(p - k0 - 4 * hi);
+    masked_block<DH, kMode, 2>(st, k_lds, v_lds, ra, ca, sc, 0, !(k0 >= sb.lo && k0 + kTok <= sa.hi), k0 + 4 * hi - seen.lo,
+                               max(0, seen.hi - seen.lo), gap);
+  }
+  if (!live) return;
+  const int64_t t = (int64_t)row0 + 32 * wave + (again(lane) & 31);
+  const float lt = half_sum(st.l);
+  const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;      // a query that sees no key: 0
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (dt * 32 + 8 * j < d.dh)
+        store4_bf16(O + t * d.ldo + head * d.dh + dt * 32 + 8 * j + 4 * hi, st.oacc[dt][4 * j] * inv, st.oacc[dt][4 * j + 1] * inv,
+                    st.oacc[dt][4 * j + 2] * inv, st.oacc[dt][4 * j + 3] * inv);
+  if (lse && hi == 0) lse[(int64_t)head * d.Tq + t] = lt > 0.0f ? st.mc * kLn2 + logf(lt) : -INFINITY;
+}
+
+// ---- backward: dq ---------------------------------------------------------------------------------------------------------------
+// x: q.k of an element -> its probability, and what the cap leaves of a gradient (1 - tanh^2)
+template <bool kCap, bool kBias>
+__device__ __forceinline__ float prob_of(float x, const Scores& sc, float lse2, float gap, float& slack) {
+  float y;
+  if constexpr (kCap) {
+    const float r = cap_half(sc, x);
+    slack = 4.0f * r * (1.0f - r);
+    y = fmaf(-2.0f * sc.a, r, sc.a) - lse2;
+  } else {
+    y = fmaf(x, sc.c, -lse2);
+  }
+  if constexpr (kBias) y = fmaf(-sc.slope, fabsf(gap), y);
+  return fast_exp2(y);
+}
+
+// 32 keys (half kt of the tiles).  The operands from LDS pass through a ring of kRing, each requested kRing - 1 matrix instructions
+// ahead, as in the dk / dv kernel, and for its reason: with all of them requested at once registers run out.
+template <int DH, bool kCap, bool kBias>
+__device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[DH / 32], const bf16x8 (&qf)[DH / 16], const bf16x8 (&dof)[DH / 16], float lse2,
+                                               float dl, uint32_t k_rows, uint32_t v_rows, uint32_t k_cols, const Scores& sc, bool masked,
+                                               int first, int len, float gap) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  typedef Tile<DH> Tl;
+  constexpr int kRing = 4;
+  bf16x8 f[kRing];
+  f32x16 s = zero16(), dp = zero16();      // rows = keys, column = query
+  auto fetch_rows = [&](int i) { f[i % kRing] = Tl::rows(i & 1 ? v_rows : k_rows, 0, i / 2); };
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i) fetch_rows(i);
+#pragma unroll
+  for (int i = 0; i < 2 * KS; ++i) {
+    if (i + kRing - 1 < 2 * KS) fetch_rows(i + kRing - 1);
+    if (i % 2 == 0) s = mfma(f[i % kRing], qf[i / 2], s);
+    else dp = mfma(f[i % kRing], dof[i / 2], dp);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    const int j = 8 * (v / 4) + v % 4;
+    float slack = 1.0f;
+    float p = prob_of<kCap, kBias>(s[v], sc, lse2, gap - static_cast<float>(j), slack);
+    dp[v] = p * (dp[v] - dl);
+    if constexpr (kCap) dp[v] *= slack;
+  }
+  if (masked) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dp[v] = static_cast<uint32_t>(first + 8 * (v / 4) + v % 4) < static_cast<uint32_t>(len) ? dp[v] : 0.0f;
+  }
+  const bf16x8 df[2] = {pack8<0>(dp), pack8<1>(dp)};
+  __builtin_amdgcn_sched_barrier(0);
+  auto fetch_cols = [&](int i) { f[i % kRing] = Tl::cols(k_cols, 0, i / DT, i % DT); };
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i) fetch_cols(i);
+#pragma unroll
+  for (int i = 0; i < 2 * DT; ++i) {
+    if (i + kRing - 1 < 2 * DT) fetch_cols(i + kRing - 1);
+    acc[i % DT] = mfma(f[i % kRing], df[i / DT], acc[i % DT]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <int DH, bool kCap, bool kBias>
+__global__ void __launch_bounds__(256, 2)
+k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
+                const bf16_t* __restrict__ O, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
+                float* __restrict__ delta, bf16_t* __restrict__ dQ) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  typedef Tile<DH> Tl;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
+  if (!plan_is(plan, tag, true)) {
+    fill_nan(dQ, d.Tq, (int64_t)d.n_q * d.dh, d.ldq);
+    return;
+  }
+  const int item = blockIdx.x / d.n_q, pair = blockIdx.x % d.n_q;
+  if (item >= word(plan + kPlanQItems)) return;
+  const int* w = plan + z.q_at + 8 * item;
+  const int row0 = word(w + 0), rows = word(w + 1), pos0 = word(w + 2), k_start = word(w + 3), k_len = word(w + 4), prefix = word(w + 5), kb0 = word(w + 6), kb1 = word(w + 7);
+  const int window = tag.w[kTagWindow];
+  const bool causal = tag.w[kTagFlags] & 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
+  const int kvh = pair % d.n_kv, head = kvh * (d.n_q / d.n_kv) + pair / d.n_kv;
+  const Scores sc = scores_of(d, head, kBias);
+
+  const int mine = min(32, rows - 32 * wave);
+  const bool live = n < mine;
+  const int p = pos0 + 32 * wave + n;
+  const Seen seen = live ? keys_of(p, k_len, prefix, window, causal) : Seen{0, 0};
+  const Seen sa = keys_of(pos0 + 32 * wave, k_len, prefix, window, causal), sb = keys_of(pos0 + 32 * wave + mine - 1, k_len, prefix, window, causal);
+  const int64_t t0 = (int64_t)row0 + 32 * wave + n;
+
+  bf16x8 qf[KS], dof[KS];
+  float lse2 = 0.0f, dl = 0.0f;
+  f32x16 acc[DT];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const bool on = live && ks * 16 + 8 * hi < d.dh;
+    const int64_t at = head * d.dh + ks * 16 + 8 * hi;
+    qf[ks] = on ? load_frag16(Q + t0 * d.ldq + at) : bf16x8{};
+    dof[ks] = on ? load_frag16(dO + t0 * d.ldo + at) : bf16x8{};
+    const bf16x8 of = on ? load_frag16(O + t0 * d.ldo + at) : bf16x8{};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dl += static_cast<float>(dof[ks][j]) * static_cast<float>(of[j]);
+  }
+  dl = half_sum(dl);
+  if (live) {
+    lse2 = lse[(int64_t)head * d.Tq + t0] * kLog2e;
+    if (hi == 0) delta[(int64_t)head * d.Tq + t0] = dl;
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
+  const int64_t kvcol = (int64_t)kvh * d.dh;
+  const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
+  const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
+  auto request = [&](int kb) {
+    const uint32_t at = lds0 + (kb & 1) * (2 * Tl::ELEMS * 2);
+    copy_tile<DH>(K, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
+    copy_tile<DH>(V, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldv, kvcol, d.dh, from_v, at + Tl::ELEMS * 2, wave, tid);
+  };
+  if (kb0 < kb1) request(kb0);
+  for (int kb = kb0; kb < kb1; ++kb) {
+    FAAR_WAIT_VMCNT(0);
+    __syncthreads();
+    if (kb + 1 < kb1) request(kb + 1);
+    const uint32_t k_lds = lds0 + (kb & 1) * (2 * Tl::ELEMS * 2), v_lds = k_lds + Tl::ELEMS * 2;
+    const int k0 = kb * kTok;
+    if (mine <= 0 || k0 >= sb.hi || k0 + kTok <= sa.lo) continue;
+    const float gap = static_cast<float>(p - k0 - 4 * hi);
+    const bool whole = k0 >= sb.lo && k0 + kTok <= sa.hi;
+    const int first = k0 + 4 * hi - seen.lo, len = max(0, seen.hi - seen.lo);
+#pragma unroll 1
+    for (int kt = 0; kt < 2; ++kt) {
+      const uint32_t half = kt * (32 * DH * 2);
+      masked_dq_tile<DH, kCap, kBias>(acc, qf, dof, lse2, dl, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
+                                      gap - 32 * kt);
+    }
+  }
+  if (!live) return;
+  const int64_t t = (int64_t)row0 + 32 * wave + (again(lane) & 31);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (dt * 32 + 8 * j < d.dh)
+        store4_bf16(dQ + t * d.ldq + head * d.dh + dt * 32 + 8 * j + 4 * hi, acc[dt][4 * j] * d.scale, acc[dt][4 * j + 1] * d.scale,
+                    acc[dt][4 * j + 2] * d.scale, acc[dt][4 * j + 3] * d.scale);
+}
+
+// ---- backward: dk, dv -----------------------------------------------------------------------------------------------------------
+// 32 queries x 32 keys; registers and rings as in the causal kernel.  first: index of the lane's first query relative to the first that
+// sees the lane's key, of `len`; gap: distance of the lane's key from the lane's first query.
+template <int DH, bool kCap, bool kBias>
+__device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[DH / 32], f32x16 (&dv)[DH / 32], const bf16x8 (&kf)[DH / 16],
+                                                const bf16x8 (&vf)[DH / 16], const float* lse_lds, const float* delta_lds, uint32_t q_rows,
+                                                uint32_t q_cols, const Scores& sc, bool masked, int first, int len, float gap, int lane) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr uint32_t kDo = Tile<DH>::ELEMS * 2;     // the dO tile follows the q tile
+  typedef Tile<DH> Tl;
+  constexpr int kRing = 3;
+  bf16x8 f[kRing];
+  f32x16 s = zero16(), dp = zero16();      // rows = queries, column = key
+  auto fetch_rows = [&](int i) { f[i % kRing] = Tl::rows(q_rows + (i & 1) * kDo, 0, i / 2); };
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i) fetch_rows(i);
+#pragma unroll
+  for (int i = 0; i < 2 * KS; ++i) {
+    if (i + kRing - 1 < 2 * KS) fetch_rows(i + kRing - 1);
+    if (i % 2 == 0) s = mfma(f[i % kRing], kf[i / 2], s);
+    else dp = mfma(f[i % kRing], vf[i / 2], dp);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = 8 * j + 4 * (lane >> 5);
+    const float4 l4 = *reinterpret_cast<const float4*>(lse_lds + row);
+    const float4 d4 = *reinterpret_cast<const float4*>(delta_lds + row);
+    const float lr[4] = {l4.x, l4.y, l4.z, l4.w}, dr[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float slack = 1.0f;
+      float p = prob_of<kCap, kBias>(s[4 * j + r], sc, lr[r] * kLog2e, gap + static_cast<float>(8 * j + r), slack);
+      s[4 * j + r] = p;
+      float g = p * (dp[4 * j + r] - dr[r]);
+      if constexpr (kCap) g *= slack;
+      dp[4 * j + r] = g;
+    }
+    if (j == 1 || kBias) __builtin_amdgcn_sched_barrier(0);
+  }
+  if (masked) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const bool ok = static_cast<uint32_t>(first + 8 * (v / 4) + v % 4) < static_cast<uint32_t>(len);
+      s[v] = ok ? s[v] : 0.0f;
+      dp[v] = ok ? dp[v] : 0.0f;
+    }
+  }
+  const bf16x8 pf[2] = {pack8<0>(s), pack8<1>(s)}, df[2] = {pack8<0>(dp), pack8<1>(dp)};
+  __builtin_amdgcn_sched_barrier(0);
+  auto fetch_cols = [&](int i) { f[i % kRing] = Tl::cols(q_cols + (i & 1 ? 0u : kDo), 0, (i / 2) & 1, i / 4); };
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i) fetch_cols(i);
+#pragma unroll
+  for (int i = 0; i < 4 * DT; ++i) {
+    if (i + kRing - 1 < 4 * DT) fetch_cols(i + kRing - 1);
+    if (i % 2 == 0) dv[i / 4] = mfma(f[i % kRing], pf[(i / 2) & 1], dv[i / 4]);
+    else dk[i / 4] = mfma(f[i % kRing], df[(i / 2) & 1], dk[i / 4]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// 64 keys of a key / value head a workgroup: wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
+// block of 64 and 2, 3 the others, and the two sums of a block of keys meet through LDS at the end
+template <int DH, bool kCap, bool kBias>
+__global__ void __launch_bounds__(256, 2)
+k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
+                 const float* __restrict__ lse, const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
+                 bf16_t* __restrict__ dK, bf16_t* __restrict__ dV) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  typedef Tile<DH> Tl;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][q, dO]
+  __shared__ __attribute__((aligned(16))) float stats[2][2][kTok];         // [stage][lse, delta]
+  if (!plan_is(plan, tag, true)) {
+    fill_nan(dK, d.Tk, (int64_t)d.n_kv * d.dh, d.ldk);
+    fill_nan(dV, d.Tk, (int64_t)d.n_kv * d.dh, d.ldv);
+    return;
+  }
+  const int item = blockIdx.x / d.n_kv, kvh = blockIdx.x % d.n_kv;
+  if (item >= word(plan + kPlanKItems)) return;
+  const int* w = plan + z.k_at + 8 * item;
+  const int row0 = word(w + 0), rows = word(w + 1), k0 = word(w + 2), q_start = word(w + 3), q_len = word(w + 4), off = word(w + 5), prefix = word(w + 6);
+  const int window = tag.w[kTagWindow];
+  const bool causal = tag.w[kTagFlags] & 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
+  const int kw = wave & 1, qw = tid >> 7, rep = d.n_q / d.n_kv;   // qw as a lane's value: it chooses between registers below
+
+  const int mine = min(32, rows - 32 * kw);            // this wavefront's keys (none: <= 0)
+  const bool live = n < mine;
+  const Seen sa = queries_of(k0 + 32 * kw, q_len, off, prefix, window, causal), sb = queries_of(k0 + 32 * kw + mine - 1, q_len, off, prefix, window, causal);
+  const int64_t t0 = (int64_t)row0 + 32 * kw + n;
+
+  bf16x8 kf[KS], vf[KS];     // second operands: column = key
+  f32x16 dk[DT], dv[DT];     // rows = dh, column = key
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const bool on = live && ks * 16 + 8 * hi < d.dh;
+    const int64_t at = kvh * d.dh + ks * 16 + 8 * hi;
+    kf[ks] = on ? load_frag16(K + t0 * d.ldk + at) : bf16x8{};
+    vf[ks] = on ? load_frag16(V + t0 * d.ldv + at) : bf16x8{};
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    dk[dt] = zero16();
+    dv[dt] = zero16();
+  }
+  // steps: query head of the group (outer) x block of 64 queries first .. end - 1 (inner)
+  const int q_lo = queries_of(k0, q_len, off, prefix, window, causal).lo, q_hi = queries_of(k0 + rows - 1, q_len, off, prefix, window, causal).hi;
+  const int first = q_lo / kTok, end = q_hi > q_lo ? (q_hi + kTok - 1) / kTok : first, steps = rep * (end - first);
+  const uint32_t lds0 = lds_addr_of(lds), from_q = Tl::of_lane(d.ldq, tid), from_o = Tl::of_lane(d.ldo, tid);
+  const uint32_t ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
+  auto request = [&](int stage, int head, int blk) {
+    const uint32_t at = lds0 + stage * (2 * Tl::ELEMS * 2);
+    const int q0 = blk * kTok;
+    copy_tile<DH>(Q, (int64_t)q_start + q0, q_len - q0, d.ldq, (int64_t)head * d.dh, d.dh, from_q, at, wave, tid);
+    copy_tile<DH>(dO, (int64_t)q_start + q0, q_len - q0, d.ldo, (int64_t)head * d.dh, d.dh, from_o, at + Tl::ELEMS * 2, wave, tid);
+    if (wave < 2)
+      dma4((wave == 0 ? lse : delta) + (int64_t)head * d.Tq + q_start + min(q0 + lane, q_len - 1),
+           __builtin_amdgcn_readfirstlane(lds_addr_of(stats[stage][wave])));
+  };
+  int head = kvh * rep, blk = first;
+  if (steps > 0) request(0, head, blk);
+  for (int it = 0; it < steps; ++it) {
+    FAAR_WAIT_VMCNT(0);
+    __syncthreads();
+    const int i0 = blk * kTok + 32 * (wave >> 1), this_head = head;
+    if (++blk == end) {
+      blk = first;
+      ++head;
+    }
+    if (it + 1 < steps) request((it + 1) & 1, head, blk);
+    if (mine <= 0 || i0 >= sb.hi || i0 + 32 <= sa.lo || i0 >= q_len) continue;
+    const Scores sc = scores_of(d, this_head, kBias);
+    const uint32_t tile = lds0 + (it & 1) * (2 * Tl::ELEMS * 2) + (wave >> 1) * (32 * DH * 2);
+    const bool whole = i0 >= sb.lo && i0 + 32 <= sa.hi;
+    const int me = again(lane), key = k0 + 32 * kw + (me & 31), at = i0 + 4 * (me >> 5);
+    const Seen seen = whole ? Seen{0, 0} : queries_of(key, q_len, off, prefix, window, causal);
+    const float* stat = &stats[it & 1][0][32 * (wave >> 1)];
+    masked_dkv_tile<DH, kCap, kBias>(dk, dv, kf, vf, stat, stat + kTok, tile + ra, tile + ca, sc, !whole, at - seen.lo, max(0, seen.hi - seen.lo),
+                                     static_cast<float>(at + off - key), lane);
+  }
+  // the two wavefronts of a block of keys: one hands over its dv and finishes dk, the other the reverse
+  f32x16* give = reinterpret_cast<f32x16*>(lds) + (size_t)wave * DT * 64 + lane;
+  const f32x16* take = reinterpret_cast<const f32x16*>(lds) + (size_t)(wave ^ 2) * DT * 64 + lane;
+  static_assert(4 * DT * 64 * sizeof(f32x16) <= sizeof(lds), "exchange fits in the stages");
+  __syncthreads();
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    f32x16 g;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) g[i] = qw == 0 ? dv[dt][i] : dk[dt][i];
+    give[dt * 64] = g;
+  }
+  __syncthreads();
+  if (!live) return;
+  const int64_t t = (int64_t)row0 + 32 * kw + (again(lane) & 31);
+  const float k = qw == 0 ? d.scale : 1.0f;
+  bf16_t* out = qw == 0 ? dK + t * d.ldk : dV + t * d.ldv;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    f32x16 r = take[dt * 64];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = (qw == 0 ? dk[dt][i] : dv[dt][i]) + r[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (dt * 32 + 8 * i < d.dh)
+        store4_bf16(out + kvh * d.dh + dt * 32 + 8 * i + 4 * hi, r[4 * i] * k, r[4 * i + 1] * k, r[4 * i + 2] * k, r[4 * i + 3] * k);
+  }
+}
+
+// ---- one token a sequence ---------------------------------------------------------------------------------------------------------
+// A workgroup takes one piece of a sequence's keys for one key / value head and up to 32 of its query heads, which are the columns of
+// the products: blocks of 128 keys, 32 a wavefront, two stages.  The four wavefronts' sums meet through LDS; a sequence of one piece is
+// done, others leave (O, maximum, denominator) of the piece in the workspace for k_masked_join.  Bound by the one pass over the cache.
+template <int DH, int kMode>
+__global__ void __launch_bounds__(256, 1)
+k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
+               PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse, float* __restrict__ part) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  typedef Tile<DH> Tl;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][2][Tl::ELEMS];   // [stage][half of the block][k, v]
+  __shared__ float ml[2][4][32];
+  if (!plan_is(plan, tag, false)) {
+    fill_nan(O, d.Tq, (int64_t)d.n_q * d.dh, d.ldo);
+    if (lse) fill_nan(lse, d.Tq * d.n_q);
+    return;
+  }
+  const int rep = d.n_q / d.n_kv, per_head = (rep + 31) / 32, cols = d.n_kv * per_head;
+  const int item = blockIdx.x / cols, kvh = blockIdx.x % cols % d.n_kv, h0 = blockIdx.x % cols / d.n_kv * 32;
+  if (item >= word(plan + kPlanQItems)) return;
+  const int* w = plan + z.q_at + 8 * item;
+  const int seq = word(w + 0), row0 = word(w + 1), keys = word(w + 2), gap0 = word(w + 3), pieces = word(w + 4);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
+  const int heads = min(32, rep - h0), head = kvh * rep + h0 + min(n, heads - 1);
+  const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped);
+
+  MaskedState<DH> st;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    st.qf[ks] = n < heads && ks * 16 + 8 * hi < d.dh ? load_frag16(Q + (int64_t)seq * d.ldq + head * d.dh + ks * 16 + 8 * hi) : bf16x8{};
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = zero16();
+  st.mc = kMode == kBounded ? sc.ref : kLowest;
+  st.l = 0.0f;
+  const int64_t kvcol = (int64_t)kvh * d.dh;
+  const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
+  const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
+  constexpr uint32_t kTile = Tl::ELEMS * 2;
+  auto request = [&](int blk) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t at = lds0 + ((blk & 1) * 2 + h) * (2 * kTile);
+      const int j0 = blk * kPieceKeys + h * kTok;
+      copy_tile<DH>(K, (int64_t)row0 + j0, keys - j0, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
+      copy_tile<DH>(V, (int64_t)row0 + j0, keys - j0, d.ldv, kvcol, d.dh, from_v, at + kTile, wave, tid);
+    }
+  };
+  const int blocks = (keys + kPieceKeys - 1) / kPieceKeys;
+  if (blocks > 0) request(0);
+  for (int blk = 0; blk < blocks; ++blk) {
+    FAAR_WAIT_VMCNT(0);
+    __syncthreads();
+    if (blk + 1 < blocks) request(blk + 1);
+    const uint32_t k_lds = lds0 + ((blk & 1) * 2 + (wave >> 1)) * (2 * kTile), v_lds = k_lds + kTile;
+    const int j0 = blk * kPieceKeys + 32 * wave;
+    if (j0 >= keys) continue;
+    const float gap = static_cast<float>(gap0 - j0 - 4 * hi);
+    masked_block<DH, kMode, 1>(st, k_lds, v_lds, ra, ca, sc, wave & 1, j0 + 32 > keys, j0 + 4 * hi, keys, gap);
+  }
+  // the wavefronts' sums on a common maximum
+  const float lt = half_sum(st.l);
+  if (hi == 0) {
+    ml[0][wave][n] = st.mc;
+    ml[1][wave][n] = lt;
+  }
+  __syncthreads();                                     // and all tiles have been read
+  float m = ml[0][0][n], l = 0.0f;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) m = fmaxf(m, ml[0][i][n]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) l += ml[1][i][n] * fast_exp2(ml[0][i][n] - m);
+  const float f = fast_exp2(st.mc - m);
+  float* sum = reinterpret_cast<float*>(lds);          // [wavefront][dh][32 heads]
+  static_assert(4 * DH * 32 * sizeof(float) <= sizeof(lds), "sums fit in the stages");
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sum[(wave * DH + dt * 32 + 8 * (v / 4) + 4 * hi + v % 4) * 32 + n] = st.oacc[dt][v] * f;
+  __syncthreads();
+  const bool done = pieces == 1;
+  if (tid < heads) {                                   // wave 0, hi 0: m and l of head n = tid
+    if (!done) {
+      float* o = part + ((int64_t)item * d.n_q + head) * (d.dh + 2) + d.dh;
+      o[0] = m;
+      o[1] = l;
+    } else if (lse) {
+      lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+    }
+  }
+  for (int i = tid; i < heads * d.dh; i += 256) {
+    const int h = i / d.dh, c = i - h * d.dh;
+    float x = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x += sum[(q * DH + c) * 32 + h];
+    const int64_t hd = kvh * rep + h0 + h;
+    if (!done) {
+      part[((int64_t)item * d.n_q + hd) * (d.dh + 2) + c] = x;
+    } else {
+      float lh = 0.0f, mh = ml[0][0][h];
+#pragma unroll
+      for (int q = 1; q < 4; ++q) mh = fmaxf(mh, ml[0][q][h]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) lh += ml[1][q][h] * fast_exp2(ml[0][q][h] - mh);
+      O[(int64_t)seq * d.ldo + hd * d.dh + c] = static_cast<bf16_t>(f32_to_bf16(lh > 0.0f ? x / lh : 0.0f));
+    }
+  }
+}
+
+// the pieces of a sequence, one query head a workgroup, in their order
+__global__ void __launch_bounds__(128)
+k_masked_join(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, bf16_t* __restrict__ O,
+              float* __restrict__ lse) {
+  if (!plan_is(plan, tag, false)) return;              // answered by the kernel before
+  const int seq = blockIdx.x / d.n_q, head = blockIdx.x % d.n_q;
+  const int first = plan[z.seq_at + 2 * seq], pieces = plan[z.seq_at + 2 * seq + 1];
+  if (pieces == 1) return;
+  const int64_t step = (int64_t)d.n_q * (d.dh + 2);
+  const float* p = part + first * step + head * (d.dh + 2);
+  float m = kLowest, l = 0.0f, x = 0.0f;
+  for (int i = 0; i < pieces; ++i) m = fmaxf(m, p[i * step + d.dh]);
+  const bool on = threadIdx.x < d.dh;
+  for (int i = 0; i < pieces; ++i) {
+    const float f = fast_exp2(p[i * step + d.dh] - m);
+    l += p[i * step + d.dh + 1] * f;
+    if (on) x += p[i * step + threadIdx.x] * f;
+  }
+  if (on) O[(int64_t)seq * d.ldo + head * d.dh + threadIdx.x] = static_cast<bf16_t>(f32_to_bf16(l > 0.0f ? x / l : 0.0f));
+  if (lse && threadIdx.x == 0) lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+}  // namespace
+
+PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, bool single) {
+  PlanSizes z{};
+  z.q_at = 16;
+  if (single) {
+    const int64_t cols = n_kv * ((n_q / n_kv + 31) / 32);
+    z.target = static_cast<int>((512 + cols - 1) / cols);
+    z.max_q = n_seq + z.target;
+    z.seq_at = static_cast<int>(z.q_at + 8 * z.max_q);
+    z.words = z.seq_at + 2 * n_seq;
+    return z;
+  }
+  z.max_q = Tq / 128 + n_seq;
+  z.max_k = Tk / kTok + n_seq;
+  z.k_at = static_cast<int>(z.q_at + 8 * z.max_q);
+  z.words = z.k_at + 8 * z.max_k;
+  return z;
+}
+
+hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int* k_start, const int* k_len, const int* prefix, const PlanTag& tag,
+                                 const PlanSizes& z, int* plan, hipStream_t st) {
+  hipLaunchKernelGGL(k_attention_plan, dim3(1), dim3(kPlanThreads), 0, st, q_start, q_len, k_start, k_len, prefix, tag, z, plan);
+  return hipGetLastError();
+}
+
+hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
+                             const MaskedDims& d, bool single, bf16_t* O, float* lse, float* part, hipStream_t st) {
+  // A capped score is at most a = cap log2(e): with exponents from 2^-110 (reference a - 110 at least, so that none is lost) to
+  // 2^40 (a <= 75) sums of 2^20 of them with any sensible value stay in range, and no running maximum is needed.
+  const int mode = d.cap_a > 0.0f ? (!d.slopes && d.cap_a <= 75.0f ? kBounded : kCapped) : d.slopes ? kBiased : kPlain;
+  const int rep = d.n_q / d.n_kv;
+  const int64_t cols = (int64_t)d.n_kv * ((rep + 31) / 32);
+  const dim3 grid(static_cast<unsigned>(single ? z.max_q * cols : z.max_q * d.n_q));
+#define FAAR_MF2(DH, M)                                                                                                              \
+  do {                                                                                                                               \
+    if (single) hipLaunchKernelGGL((k_masked_token<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, part);         \
+    else hipLaunchKernelGGL((k_masked_fwd<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse);                        \
+  } while (0)
+#define FAAR_MF(M) do { if (d.dh <= 64) FAAR_MF2(64, M); else FAAR_MF2(128, M); } while (0)
+  switch (mode) {
+    case kPlain: FAAR_MF(kPlain); break;
+    case kBiased: FAAR_MF(kBiased); break;
+    case kBounded: FAAR_MF(kBounded); break;
+    default: FAAR_MF(kCapped); break;
+  }
+#undef FAAR_MF
+#undef FAAR_MF2
+  if (hipError_t e = hipGetLastError()) return e;
+  if (single && d.Tk > kPieceKeys)                     // no more keys than a block: no sequence has a second piece
+    hipLaunchKernelGGL(k_masked_join, dim3(static_cast<unsigned>(d.Tq * d.n_q)), dim3(128), 0, st, plan, tag, z, d, part, O, lse);
+  return hipGetLastError();
+}
+
+hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const float* lse,
+                             const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
+                             bf16_t* dV, hipStream_t st) {
+  const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv));
+#define FAAR_MB2(DH, C, B)                                                                                                            \
+  do {                                                                                                                                \
+    hipLaunchKernelGGL((k_masked_bwd_dq<DH, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, lse, plan, tag, z, d, delta, dQ);           \
+    hipLaunchKernelGGL((k_masked_bwd_dkv<DH, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV);         \
+  } while (0)
+#define FAAR_MB(C, B) do { if (d.dh <= 64) FAAR_MB2(64, C, B); else FAAR_MB2(128, C, B); } while (0)
+  if (d.cap_a > 0.0f) { if (d.slopes) FAAR_MB(true, true); else FAAR_MB(true, false); }
+  else                { if (d.slopes) FAAR_MB(false, true); else FAAR_MB(false, false); }
+#undef FAAR_MB
+#undef FAAR_MB2
+  return hipGetLastError();
+}
+
+}  // namespace faar
