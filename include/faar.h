@@ -710,16 +710,18 @@ size_t faar_attention_masked_workspace_bytes(const faar_attention* a, int32_t ba
  * n_q, n_kv and the same form until the lengths it was made from change. */
 int faar_attention_plan(const faar_attention* a, void* plan, size_t plan_bytes, void* stream);
 
-/* q in bf16 [Tq] rows of n_q * dh, k, v in bf16 [Tk] rows of n_kv * dh, o out bf16; lse out, nullable float [n_q * Tq] (kept for the
- * backward).  float32 arithmetic; probabilities are rounded to bf16 as matrix-core operands. */
+/* q in bf16 [Tq] rows of n_q * dh, k, v in bf16 [Tk] rows of n_kv * dh, o out bf16; kept for the backward: lse out, nullable float [n_q * Tq],
+ * and o_low out, nullable int8 [Tq][n_q * dh]: what the rounding took from o, in 2^-8 of its last place (not with single tokens).
+ * float32 arithmetic; probabilities are rounded to bf16 as matrix-core operands. */
 int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* q, const void* k, const void* v, void* o,
-                              float* lse, void* ws, size_t ws_bytes, void* stream);
+                              float* lse, uint8_t* o_low, void* ws, size_t ws_bytes, void* stream);
 
-/* (dq, dk, dv) for the output gradient d_o; o and lse from the forward call.  dk and dv are summed over the query heads of a group in
- * a fixed order.  Outputs must not overlap inputs. */
+/* (dq, dk, dv) for the output gradient d_o; o, lse and o_low from the forward call.  o_low may be NULL: the gradients of queries whose
+ * softmax is sharp then carry the rounding of o, many times over.  dk and dv are summed over the query heads of a group in a fixed
+ * order.  Outputs must not overlap inputs. */
 int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* d_o, const void* q, const void* k,
-                              const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
-                              void* stream);
+                              const void* v, const void* o, const float* lse, const uint8_t* o_low, void* dq, void* dk, void* dv, void* ws,
+                              size_t ws_bytes, void* stream);
 
 /* a = SiLU(p) q = p sigmoid(p) q, all bf16 [n], n % 8 == 0 */
 int faar_silu_mul_fwd(const void* p, const void* q, int64_t n, void* a, void* stream);

@@ -8,6 +8,6 @@ from .binding import (FaarError, faar_adam, faar_harden_pack, faar_hardened_loss
                       faar_init_v_batch, faar_harden_pack_batch, faar_linear_forward, faar_rmsnorm_fwd, faar_rmsnorm_bwd,
                       faar_silu_mul_fwd, faar_silu_mul_bwd, faar_block_output_loss, faar_residual_add, faar_rope, block_description, faar_block_workspace, faar_block_joint_step, faar_attention_fwd, faar_attention_bwd,
                       faar_layernorm_fwd, faar_layernorm_bwd, layernorm_workspace, faar_rope_axes,
-                      attention_description, attention_masked_workspace, faar_attention_plan, faar_attention_masked_fwd,
+                      AttentionStats, attention_description, attention_masked_workspace, faar_attention_plan, faar_attention_masked_fwd,
                       faar_attention_masked_bwd,
                       faar_stage2_losses, faar_workspace_bytes, layer_step_workspace, lib)

@@ -165,10 +165,11 @@ def lib() -> ctypes.CDLL:
         L.faar_attention_plan.restype = c_int
         L.faar_attention_plan.argtypes = [A, c_void_p, c_size_t, c_void_p]
         L.faar_attention_masked_fwd.restype = c_int
-        L.faar_attention_masked_fwd.argtypes = [A, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.faar_attention_masked_fwd.argtypes = [A, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                                c_void_p]
         L.faar_attention_masked_bwd.restype = c_int
         L.faar_attention_masked_bwd.argtypes = [A, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
-                                                c_void_p, c_void_p, c_size_t, c_void_p]
+                                                c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         L.faar_rope_axes.restype = c_int
         L.faar_rope_axes.argtypes = [c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int64, c_int64, c_void_p, c_int64,
                                      c_void_p, c_void_p, c_uint32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
@@ -723,44 +724,60 @@ def attention_masked_workspace(a, backward=False):
     return torch.empty(n, dtype=torch.uint8, device=a._device)
 
 
-def _masked_rows(a, where, q, k, v, o, lse=None):
+class AttentionStats:
+    """What a forward call keeps for its backward: lse float32 [n_q, Tq] and the low bytes of o, int8 [Tq, n_q * dh]."""
+    __slots__ = ("lse", "o_low")
+
+    def __init__(self, lse, o_low):
+        self.lse, self.o_low = lse, o_low
+
+
+def _masked_rows(a, where, q, k, v, o, stats):
     _rows(where, q=q, k=k, v=v, o=o)
-    _dev(lse)
     kv = (a.Tk, a.n_kv * a.dh)
-    if q.shape != (a.Tq, a.n_q * a.dh) or o.shape != q.shape or k.shape != kv or v.shape != kv or \
-            (lse is not None and (lse.dtype != torch.float32 or lse.numel() != a.n_q * a.Tq)):
-        raise ValueError(f"{where}: q, o [Tq, n_q * dh]; k, v [Tk, n_kv * dh]; lse float32 [n_q, Tq]")
+    if q.shape != (a.Tq, a.n_q * a.dh) or o.shape != q.shape or k.shape != kv or v.shape != kv:
+        raise ValueError(f"{where}: q, o [Tq, n_q * dh]; k, v [Tk, n_kv * dh]")
+    if stats is not None:
+        _dev(stats.lse, stats.o_low)
+        if stats.lse.dtype != torch.float32 or stats.lse.numel() != a.n_q * a.Tq or \
+                (stats.o_low is not None and (stats.o_low.dtype != torch.int8 or stats.o_low.shape != q.shape)):
+            raise ValueError(f"{where}: lse float32 [n_q, Tq], o_low int8 [Tq, n_q * dh]")
     d = faar_attention.from_buffer_copy(a)               # the caller's description may be in use by another thread
     d.ldq, d.ldk, d.ldv, d.ldo = _ld(q), _ld(k), _ld(v), _ld(o)
     return d
 
 
 def faar_attention_masked_fwd(a, plan, q, k, v, out=None, want_lse=True, ws=None):
-    """-> (o bf16 [Tq, n_q * dh], lse float32 [n_q, Tq] or None).  Rows of no sequence keep what out holds (0 where out is not given)."""
+    """-> (o bf16 [Tq, n_q * dh], stats for the backward (stats.lse float32 [n_q, Tq]), or None without want_lse).  Rows of no sequence
+    keep what out holds (0 where out is not given)."""
     o = torch.zeros((a.Tq, a.n_q * a.dh), dtype=torch.bfloat16, device=q.device) if out is None else out
-    lse = torch.empty((a.n_q, a.Tq), dtype=torch.float32, device=q.device) if want_lse else None
-    d = _masked_rows(a, "faar_attention_masked_fwd", q, k, v, o)
+    stats = None
+    if want_lse:
+        single = a.q_len is None
+        stats = AttentionStats(torch.empty((a.n_q, a.Tq), dtype=torch.float32, device=q.device),
+                               None if single else torch.empty((a.Tq, a.n_q * a.dh), dtype=torch.int8, device=q.device))
+    d = _masked_rows(a, "faar_attention_masked_fwd", q, k, v, o, stats)
     ws = attention_masked_workspace(a) if ws is None else ws
     _dev(plan, ws)
-    _check(lib().faar_attention_masked_fwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(ws),
-                                           ws.numel(), _stream()), "faar_attention_masked_fwd")
-    return o, lse
+    _check(lib().faar_attention_masked_fwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+                                           _ptr(stats.lse) if stats else None, _ptr(stats.o_low) if stats else None, _ptr(ws), ws.numel(),
+                                           _stream()), "faar_attention_masked_fwd")
+    return o, stats
 
 
-def faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, lse, out=None, ws=None):
+def faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, out=None, ws=None):
     """-> (dq, dk, dv) bf16, shaped like q, k, v (out: the same three, with the row strides of q, k and v).  Rows of no sequence keep what
     out holds (0 where out is not given)."""
-    if out is None:
-        out = tuple(_zeros_like_rows(t) for t in (q, k, v))
-    dq, dk, dv = out
-    d = _masked_rows(a, "faar_attention_masked_bwd", q, k, v, o, lse)
+    dq, dk, dv = tuple(_zeros_like_rows(t) for t in (q, k, v)) if out is None else out
+    d = _masked_rows(a, "faar_attention_masked_bwd", q, k, v, o, stats)
     _rows("faar_attention_masked_bwd", d_o=d_o, dq=dq, dk=dk, dv=dv)
     if any(x.shape != y.shape or _ld(x) != _ld(y) for x, y in ((d_o, o), (dq, q), (dk, k), (dv, v))):
         raise ValueError("faar_attention_masked_bwd: gradients have the shapes and row strides of what they belong to")
     ws = attention_masked_workspace(a, backward=True) if ws is None else ws
     _dev(plan, ws)
-    _check(lib().faar_attention_masked_bwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
-                                           _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()), "faar_attention_masked_bwd")
+    _check(lib().faar_attention_masked_bwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+                                           _ptr(stats.lse), _ptr(stats.o_low), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()),
+           "faar_attention_masked_bwd")
     return dq, dk, dv
 
 

@@ -1038,7 +1038,7 @@ int masked_rows(const faar_attention* a) {
 
 size_t masked_ws_bytes(const MaskedCall& c, bool backward) {
   if (backward) return align256((size_t)c.d.n_q * c.d.Tq * sizeof(float));        // rowsum(dO o) per head and query
-  if (c.single) return align256((size_t)c.z.max_q * c.d.n_q * (c.d.dh + 2) * sizeof(float));
+  if (c.single) return align256((size_t)c.z.max_q * c.d.n_q * (c.d.dh + kPartExtra) * sizeof(float));
   return 256;                                          // none needed
 }
 
@@ -1066,35 +1066,36 @@ int faar_attention_plan(const faar_attention* a, void* plan, size_t plan_bytes, 
 }
 
 int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* q, const void* k, const void* v, void* o,
-                              float* lse, void* ws, size_t ws_bytes, void* stream) {
+                              float* lse, uint8_t* o_low, void* ws, size_t ws_bytes, void* stream) {
   if (!a || !plan || !q || !k || !v || !o) return FAAR_E_NULL;
   MaskedCall c;
   if (int e = masked_call(a, c)) return e;
+  if (c.single && o_low) return FAAR_E_UNSUPPORTED;
   if (int e = masked_rows(a)) return e;
-  if (!aligned16(plan) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(ws) ||
+  if (!aligned16(plan) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_low) || !aligned16(ws) ||
       (reinterpret_cast<uintptr_t>(lse) & 3u))
     return FAAR_E_ARG;
   if (plan_bytes < align256((size_t)c.z.words * 4) || !ws || ws_bytes < masked_ws_bytes(c, false)) return FAAR_E_WORKSPACE;
   return hip_status(launch_masked_fwd(static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v),
-                                      static_cast<const int*>(plan), c.tag, c.z, c.d, c.single, static_cast<bf16_t*>(o), lse,
+                                      static_cast<const int*>(plan), c.tag, c.z, c.d, c.single, static_cast<bf16_t*>(o), lse, o_low,
                                       static_cast<float*>(ws), static_cast<hipStream_t>(stream)));
 }
 
 int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* d_o, const void* q, const void* k,
-                              const void* v, const void* o, const float* lse, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
-                              void* stream) {
+                              const void* v, const void* o, const float* lse, const uint8_t* o_low, void* dq, void* dk, void* dv, void* ws,
+                              size_t ws_bytes, void* stream) {
   if (!a || !plan || !d_o || !q || !k || !v || !o || !lse || !dq || !dk || !dv) return FAAR_E_NULL;
   MaskedCall c;
   if (int e = masked_call(a, c)) return e;
   if (c.single) return FAAR_E_UNSUPPORTED;
   if (int e = masked_rows(a)) return e;
-  for (const void* p : {plan, d_o, q, k, v, o, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(ws)})
+  for (const void* p : {plan, d_o, q, k, v, o, static_cast<const void*>(o_low), static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(ws)})
     if (!aligned16(p)) return FAAR_E_ARG;
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return FAAR_E_ARG;
   if (plan_bytes < align256((size_t)c.z.words * 4) || !ws || ws_bytes < masked_ws_bytes(c, true)) return FAAR_E_WORKSPACE;
   return hip_status(launch_masked_bwd(static_cast<const bf16_t*>(d_o), static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k),
-                                      static_cast<const bf16_t*>(v), static_cast<const bf16_t*>(o), lse, static_cast<const int*>(plan), c.tag, c.z,
-                                      c.d, static_cast<float*>(ws), static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk), static_cast<bf16_t*>(dv),
+                                      static_cast<const bf16_t*>(v), static_cast<const bf16_t*>(o), o_low, lse, static_cast<const int*>(plan), c.tag,
+                                      c.z, c.d, static_cast<float*>(ws), static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk), static_cast<bf16_t*>(dv),
                                       static_cast<hipStream_t>(stream)));
 }
 

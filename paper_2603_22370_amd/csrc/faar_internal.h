@@ -204,11 +204,13 @@ struct MaskedDims {
 PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, bool single);
 hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int* k_start, const int* k_len, const int* prefix, const PlanTag& tag,
                                  const PlanSizes& z, int* plan, hipStream_t st);
-// part (single tokens): [max_q][n_q][dh + 2]
+// part (single tokens): [max_q][n_q][dh + kPartExtra]: a piece's sum, maximum and two denominators
+constexpr int kPartExtra = 3;
+// o_low: nullable [Tq][n_q * dh], the 8 bits behind each bf16 of O (forward out, not with single tokens; backward in)
 hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
-                             const MaskedDims& d, bool single, bf16_t* O, float* lse, float* part, hipStream_t st);
+                             const MaskedDims& d, bool single, bf16_t* O, float* lse, uint8_t* o_low, float* part, hipStream_t st);
 // delta: [n_q][Tq]
-hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const float* lse,
+hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
                              const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st);
 // lse [n_q, T]

@@ -16,8 +16,14 @@
 //
 // Tiles, copies and products are those of the causal kernels (faar_attention.hip): 64-token tiles in LDS by asynchronous copies, two
 // stages, 32 queries (keys) a wavefront, v_mfma_f32_32x32x16_bf16, probabilities in the accumulator layout as the next operand.
-// P and dz are rounded to bf16 as matrix-core operands, like there: half the cost of the products' time is what exact ones would add
-// in a second product each, and the outputs are bf16.  Everything else is float32.
+// P and dz are rounded to bf16 as matrix-core operands, like there: exact ones would be a second product each, and the outputs are
+// bf16.  Everything else is float32, and what a rounding would do where a softmax is sharp is kept out of it: there dP - rowsum(dO o)
+// is a small difference of large numbers, and rowsum has to be the mean of dP under P to more than the digits of bf16.
+//   * o is divided by the sum of the ROUNDED probabilities (lse keeps that of the others): its error is then sum P eps (v - o) instead of
+//     sum P eps v, as small as the difference itself.  A dot product of two pairs adds two rounded probabilities per instruction.
+//   * next to o the forward can leave the 8 bits that follow each of its bf16 values (o_low), and the backward takes o to 16 significant bits.
+// Norm-wise error of dq against 64 bits on 13 sequences whose scores have a deviation of 9 (10007 queries, 16 heads of 80): without the two
+// 7.4e-3.
 #include <algorithm>
 
 #include "faar_attention_tile.h"
@@ -262,8 +268,14 @@ template <int DH>
 struct MaskedState {
   bf16x8 qf[DH / 16];
   f32x16 oacc[DH / 32];   // rows = dh, column = query lane % 32
-  float mc, l;            // reference maximum (units of log 2), and this half-wave's share of the denominator
+  float mc, l, lr;        // reference maximum (units of log 2), this half-wave's share of the denominator, and that of rounded probabilities
 };
+
+// a + the two bf16 of w
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float add_pair(uint32_t w, float a) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), a, false);
+}
 
 // NT x 32 keys of tiles at k_lds, v_lds (first 32: half `h0`).  first: index of the lane's first key relative to what is compared:
 // `len` keys from 0 on are seen (masked); gap: distance of the lane's first key from its query.
@@ -312,6 +324,7 @@ __device__ __forceinline__ void masked_block(MaskedState<DH>& st, uint32_t k_lds
       const float alpha = fast_exp2(st.mc - nm);
       st.mc = nm;
       st.l *= alpha;
+      st.lr *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) st.oacc[dt] *= alpha;
     }
@@ -331,18 +344,38 @@ __device__ __forceinline__ void masked_block(MaskedState<DH>& st, uint32_t k_lds
   st.l += ps;
 #pragma unroll
   for (int kt = 0; kt < NT; ++kt) {
-    const bf16x8 p0 = pack8<0>(s[kt]), p1 = pack8<1>(s[kt]);
+    Frag p0, p1;
+    p0.v = pack8<0>(s[kt]);
+    p1.v = pack8<1>(s[kt]);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 0, dt), p0, st.oacc[dt]);
+    for (int i = 0; i < 4; ++i) st.lr = add_pair(p1.w[i], add_pair(p0.w[i], st.lr));
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 1, dt), p1, st.oacc[dt]);
+    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 0, dt), p0.v, st.oacc[dt]);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 1, dt), p1.v, st.oacc[dt]);
   }
+}
+
+// what rounding four floats to bf16 (w) took from them, in units of 2^-8 of the last place: a signed byte each
+__device__ __forceinline__ uint32_t low_bytes(const float (&x)[4], const uint2& w) {
+  const uint32_t top[4] = {w.x << 16, w.x & 0xFFFF0000u, w.y << 16, w.y & 0xFFFF0000u};
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int off = static_cast<int>(__float_as_uint(x[i]) - top[i]);            // -2^15 .. 2^15
+    r |= static_cast<uint32_t>(min(127, (off + 128) >> 8) & 0xFF) << (8 * i);
+  }
+  return r;
+}
+// the float of a bf16 and its byte
+__device__ __forceinline__ float with_low(uint32_t bf16_top, uint32_t byte) {
+  return __uint_as_float(bf16_top + (static_cast<uint32_t>(static_cast<int>(byte << 24) >> 24) << 8));
 }
 
 template <int DH, int kMode>
 __global__ void __launch_bounds__(256, 2)
 k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
-             PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse) {
+             PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse, uint8_t* __restrict__ o_low) {
   constexpr int KS = DH / 16, DT = DH / 32;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
@@ -374,7 +407,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = zero16();
   st.mc = kMode == kBounded ? sc.ref : kLowest;
-  st.l = 0.0f;
+  st.l = st.lr = 0.0f;
   const int64_t kvcol = (int64_t)kvh * d.dh;
   const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
   const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
@@ -397,15 +430,21 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
   }
   if (!live) return;
   const int64_t t = (int64_t)row0 + 32 * wave + (again(lane) & 31);
-  const float lt = half_sum(st.l);
-  const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;      // a query that sees no key: 0
+  const float lt = half_sum(st.l), lr = half_sum(st.lr);
+  const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;      // a query that sees no key: 0
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (dt * 32 + 8 * j < d.dh)
-        store4_bf16(O + t * d.ldo + head * d.dh + dt * 32 + 8 * j + 4 * hi, st.oacc[dt][4 * j] * inv, st.oacc[dt][4 * j + 1] * inv,
-                    st.oacc[dt][4 * j + 2] * inv, st.oacc[dt][4 * j + 3] * inv);
+      if (dt * 32 + 8 * j < d.dh) {
+        const int c = head * d.dh + dt * 32 + 8 * j + 4 * hi;
+        float x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = st.oacc[dt][4 * j + r] * inv;
+        const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        *reinterpret_cast<uint2*>(O + t * d.ldo + c) = w;
+        if (o_low) *reinterpret_cast<uint32_t*>(o_low + t * ((int64_t)d.n_q * d.dh) + c) = low_bytes(x, w);
+      }
   if (lse && hi == 0) lse[(int64_t)head * d.Tq + t] = lt > 0.0f ? st.mc * kLn2 + logf(lt) : -INFINITY;
 }
 
@@ -474,7 +513,7 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[DH / 32], const bf1
 template <int DH, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
-                const bf16_t* __restrict__ O, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
+                const bf16_t* __restrict__ O, const uint8_t* __restrict__ o_low, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
                 float* __restrict__ delta, bf16_t* __restrict__ dQ) {
   constexpr int KS = DH / 16, DT = DH / 32;
   typedef Tile<DH> Tl;
@@ -509,9 +548,13 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
     const int64_t at = head * d.dh + ks * 16 + 8 * hi;
     qf[ks] = on ? load_frag16(Q + t0 * d.ldq + at) : bf16x8{};
     dof[ks] = on ? load_frag16(dO + t0 * d.ldo + at) : bf16x8{};
-    const bf16x8 of = on ? load_frag16(O + t0 * d.ldo + at) : bf16x8{};
+    Frag of;
+    of.v = on ? load_frag16(O + t0 * d.ldo + at) : bf16x8{};
+    uint2 low = make_uint2(0, 0);
+    if (on && o_low) low = *reinterpret_cast<const uint2*>(o_low + t0 * ((int64_t)d.n_q * d.dh) + at);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dl += static_cast<float>(dof[ks][j]) * static_cast<float>(of[j]);
+    for (int j = 0; j < 8; ++j)
+      dl += static_cast<float>(dof[ks][j]) * with_low(j & 1 ? of.w[j / 2] & 0xFFFF0000u : of.w[j / 2] << 16, (j < 4 ? low.x : low.y) >> (8 * (j & 3)));
   }
   dl = half_sum(dl);
   if (live) {
@@ -738,7 +781,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
   constexpr int KS = DH / 16, DT = DH / 32;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][2][Tl::ELEMS];   // [stage][half of the block][k, v]
-  __shared__ float ml[2][4][32];
+  __shared__ float ml[3][4][32];
   if (!plan_is(plan, tag, false)) {
     fill_nan(O, d.Tq, (int64_t)d.n_q * d.dh, d.ldo);
     if (lse) fill_nan(lse, d.Tq * d.n_q);
@@ -760,7 +803,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = zero16();
   st.mc = kMode == kBounded ? sc.ref : kLowest;
-  st.l = 0.0f;
+  st.l = st.lr = 0.0f;
   const int64_t kvcol = (int64_t)kvh * d.dh;
   const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
   const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
@@ -787,17 +830,27 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
     masked_block<DH, kMode, 1>(st, k_lds, v_lds, ra, ca, sc, wave & 1, j0 + 32 > keys, j0 + 4 * hi, keys, gap);
   }
   // the wavefronts' sums on a common maximum
-  const float lt = half_sum(st.l);
+  const float lt = half_sum(st.l), lr = half_sum(st.lr);
   if (hi == 0) {
     ml[0][wave][n] = st.mc;
     ml[1][wave][n] = lt;
+    ml[2][wave][n] = lr;
   }
   __syncthreads();                                     // and all tiles have been read
-  float m = ml[0][0][n], l = 0.0f;
+  auto joined = [&](int h, float& m, float& l, float& r) {
+    m = ml[0][0][h];
+    l = r = 0.0f;
 #pragma unroll
-  for (int i = 1; i < 4; ++i) m = fmaxf(m, ml[0][i][n]);
+    for (int i = 1; i < 4; ++i) m = fmaxf(m, ml[0][i][h]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) l += ml[1][i][n] * fast_exp2(ml[0][i][n] - m);
+    for (int i = 0; i < 4; ++i) {
+      const float f = fast_exp2(ml[0][i][h] - m);
+      l += ml[1][i][h] * f;
+      r += ml[2][i][h] * f;
+    }
+  };
+  float m, l, r;
+  joined(n, m, l, r);
   const float f = fast_exp2(st.mc - m);
   float* sum = reinterpret_cast<float*>(lds);          // [wavefront][dh][32 heads]
   static_assert(4 * DH * 32 * sizeof(float) <= sizeof(lds), "sums fit in the stages");
@@ -809,9 +862,10 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
   const bool done = pieces == 1;
   if (tid < heads) {                                   // wave 0, hi 0: m and l of head n = tid
     if (!done) {
-      float* o = part + ((int64_t)item * d.n_q + head) * (d.dh + 2) + d.dh;
+      float* o = part + ((int64_t)item * d.n_q + head) * (d.dh + kPartExtra) + d.dh;
       o[0] = m;
       o[1] = l;
+      o[2] = r;
     } else if (lse) {
       lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
     }
@@ -823,14 +877,11 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
     for (int q = 0; q < 4; ++q) x += sum[(q * DH + c) * 32 + h];
     const int64_t hd = kvh * rep + h0 + h;
     if (!done) {
-      part[((int64_t)item * d.n_q + hd) * (d.dh + 2) + c] = x;
+      part[((int64_t)item * d.n_q + hd) * (d.dh + kPartExtra) + c] = x;
     } else {
-      float lh = 0.0f, mh = ml[0][0][h];
-#pragma unroll
-      for (int q = 1; q < 4; ++q) mh = fmaxf(mh, ml[0][q][h]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) lh += ml[1][q][h] * fast_exp2(ml[0][q][h] - mh);
-      O[(int64_t)seq * d.ldo + hd * d.dh + c] = static_cast<bf16_t>(f32_to_bf16(lh > 0.0f ? x / lh : 0.0f));
+      float mh, lh, rh;
+      joined(h, mh, lh, rh);
+      O[(int64_t)seq * d.ldo + hd * d.dh + c] = static_cast<bf16_t>(f32_to_bf16(rh > 0.0f ? x / rh : 0.0f));
     }
   }
 }
@@ -843,17 +894,18 @@ k_masked_join(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims
   const int seq = blockIdx.x / d.n_q, head = blockIdx.x % d.n_q;
   const int first = plan[z.seq_at + 2 * seq], pieces = plan[z.seq_at + 2 * seq + 1];
   if (pieces == 1) return;
-  const int64_t step = (int64_t)d.n_q * (d.dh + 2);
-  const float* p = part + first * step + head * (d.dh + 2);
-  float m = kLowest, l = 0.0f, x = 0.0f;
+  const int64_t step = (int64_t)d.n_q * (d.dh + kPartExtra);
+  const float* p = part + first * step + head * (d.dh + kPartExtra);
+  float m = kLowest, l = 0.0f, r = 0.0f, x = 0.0f;
   for (int i = 0; i < pieces; ++i) m = fmaxf(m, p[i * step + d.dh]);
   const bool on = threadIdx.x < d.dh;
   for (int i = 0; i < pieces; ++i) {
     const float f = fast_exp2(p[i * step + d.dh] - m);
     l += p[i * step + d.dh + 1] * f;
+    r += p[i * step + d.dh + 2] * f;
     if (on) x += p[i * step + threadIdx.x] * f;
   }
-  if (on) O[(int64_t)seq * d.ldo + head * d.dh + threadIdx.x] = static_cast<bf16_t>(f32_to_bf16(l > 0.0f ? x / l : 0.0f));
+  if (on) O[(int64_t)seq * d.ldo + head * d.dh + threadIdx.x] = static_cast<bf16_t>(f32_to_bf16(r > 0.0f ? x / r : 0.0f));
   if (lse && threadIdx.x == 0) lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
 }
 
@@ -884,7 +936,7 @@ hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int
 }
 
 hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
-                             const MaskedDims& d, bool single, bf16_t* O, float* lse, float* part, hipStream_t st) {
+                             const MaskedDims& d, bool single, bf16_t* O, float* lse, uint8_t* o_low, float* part, hipStream_t st) {
   // A capped score is at most a = cap log2(e): with exponents from 2^-110 (reference a - 110 at least, so that none is lost) to
   // 2^40 (a <= 75) sums of 2^20 of them with any sensible value stay in range, and no running maximum is needed.
   const int mode = d.cap_a > 0.0f ? (!d.slopes && d.cap_a <= 75.0f ? kBounded : kCapped) : d.slopes ? kBiased : kPlain;
@@ -894,7 +946,7 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
 #define FAAR_MF2(DH, M)                                                                                                              \
   do {                                                                                                                               \
     if (single) hipLaunchKernelGGL((k_masked_token<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, part);         \
-    else hipLaunchKernelGGL((k_masked_fwd<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse);                        \
+    else hipLaunchKernelGGL((k_masked_fwd<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, o_low);                 \
   } while (0)
 #define FAAR_MF(M) do { if (d.dh <= 64) FAAR_MF2(64, M); else FAAR_MF2(128, M); } while (0)
   switch (mode) {
@@ -911,13 +963,13 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
   return hipGetLastError();
 }
 
-hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const float* lse,
+hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
                              const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st) {
   const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv));
 #define FAAR_MB2(DH, C, B)                                                                                                            \
   do {                                                                                                                                \
-    hipLaunchKernelGGL((k_masked_bwd_dq<DH, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, lse, plan, tag, z, d, delta, dQ);           \
+    hipLaunchKernelGGL((k_masked_bwd_dq<DH, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ);    \
     hipLaunchKernelGGL((k_masked_bwd_dkv<DH, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV);         \
   } while (0)
 #define FAAR_MB(C, B) do { if (d.dh <= 64) FAAR_MB2(64, C, B); else FAAR_MB2(128, C, B); } while (0)

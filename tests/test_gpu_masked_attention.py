@@ -6,8 +6,10 @@ matrix cores' sum, the cap's exponential and reciprocal, the bias), so its proba
 bf16, and so is every output:
     o:   U8 |o| + (U8 + 2 e) sum P |v|
     dv:  U8 |dv| + sum (U8 + 2 e) P |dO|,  over the query heads that share the key / value head
-    ds = P (dP - delta) slack is good to (U8 + 4 e) |ds| and to what delta, from the stored o, is off by: P slack sum |dO| tol(o); dq and dk
-    sum that over keys and queries, times scale |k| and scale |q|.
+    ds = P (dP - delta) slack is good to (U8 + 4 e) |ds| and to what delta is off by, times P slack; dq and dk sum that over keys and
+    queries, times scale |k| and scale |q|.  delta = sum dO o: without the low bytes of o off by sum |dO| tol(o).  With them o is
+    sum w v / sum w with weights P (1 + eps), |eps| <= U8 + 2 e, off by sum P eps (v - o) up to second order, and stored to 2^-15: delta
+    is off by 1.02 (U8 + 2 e) sum P |dP - delta| + 2^-15 sum |dO| |o| and float32 sums of dh products, 64 u sum |dO| sum P |v|.
 Denominators and the sums over keys run in float32 over at most a few thousand terms of one sign in 16 or more partial sums: below
 1e-5, in e."""
 import ctypes
@@ -42,7 +44,7 @@ def ints(a):
     return torch.tensor(list(a), dtype=torch.int32, device="cuda")
 
 
-def tolerances(q, k, v, seqs, n_q, n_kv, dh, scale, causal, window, cap, slopes, d_o=None):
+def tolerances(q, k, v, seqs, n_q, n_kv, dh, scale, causal, window, cap, slopes, d_o=None, low=True):
     rep = n_q // n_kv
     tol = {"o": np.zeros_like(q), "lse": np.zeros((n_q, q.shape[0])), "dq": np.zeros_like(q), "dk": np.zeros_like(k), "dv": np.zeros_like(v)}
     want = bo.masked_attention(q, k, v, seqs, n_q, n_kv, dh, scale, causal, window, cap, slopes, d_o)
@@ -126,9 +128,9 @@ class Case:
                                        slopes=None if self.slopes is None else torch.from_numpy(self.slopes).cuda())
         return a, parts
 
-    def oracle(self, grad=True):
+    def oracle(self, grad=True, low=True):
         return tolerances(self.q, self.k, self.v, self.seqs, self.n_q, self.n_kv, self.dh, self.scale, self.causal, self.window, self.cap, self.slopes,
-                          self.d_o if grad else None)
+                          self.d_o if grad else None, low)
 
 
 def packed(lens, prefix=0, gap=0):
@@ -215,20 +217,24 @@ def test_forward_and_backward(name):
     plan = faar.faar_attention_plan(a)
     ws = faar.attention_masked_workspace(a, backward=True)
     out = torch.full((c.Tq, c.n_q * c.dh), 7.0, dtype=torch.bfloat16, device="cuda")
-    o, lse = faar.faar_attention_masked_fwd(a, plan, q, k, v, out=out, ws=ws)
+    o, stats = faar.faar_attention_masked_fwd(a, plan, q, k, v, out=out, ws=ws)
     rows, keys = c.q_rows, c.k_rows
     assert (host(o)[~rows] == 7.0).all()                   # rows of no sequence are left as they were
     inside(host(o)[rows], o_w[rows], tol["o"][rows], "o")
-    got = host(lse)[:, rows]
+    got = host(stats.lse)[:, rows]
     none = np.isneginf(lse_w[:, rows])
     assert np.array_equal(np.isneginf(got), none)
     inside(got[~none], lse_w[:, rows][~none], tol["lse"][:, rows][~none], "lse")
     assert not host(o)[rows][none.any(axis=0)].any()       # a query that sees no key
-    grads = [fb._zeros_like_rows(t).fill_(7.0) for t in (q, k, v)]
-    grads = faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, lse, out=grads, ws=ws)
-    for g, w, r, n in zip(grads, (dq_w, dk_w, dv_w), (rows, keys, keys), ("dq", "dk", "dv")):
-        assert (host(g)[~r] == 7.0).all(), n
-        inside(host(g)[r], w[r], tol[n][r], n)
+    for low in (True, False):
+        if not low:
+            stats, (_, tol) = faar.AttentionStats(stats.lse, None), c.oracle(low=False)
+        grads = [fb._zeros_like_rows(t).fill_(7.0) for t in (q, k, v)]
+        grads = faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, out=grads, ws=ws)
+        for g, w, r, n in zip(grads, (dq_w, dk_w, dv_w), (rows, keys, keys), ("dq", "dk", "dv")):
+            assert (host(g)[~r] == 7.0).all(), n
+            inside(host(g)[r], w[r], tol[n][r], n)
+
 
 
 TOKENS = {  # lengths of the caches, capacity, n_q, n_kv, dh, window, cap, slopes
@@ -282,11 +288,11 @@ def test_single_tokens(name):
             at += keys
         assert at == b * cap_rows + L
         first += len(mine)
-    o, lse = faar.faar_attention_masked_fwd(a, plan, dev(q), kd, vd)
+    o, stats = faar.faar_attention_masked_fwd(a, plan, dev(q), kd, vd)
     inside(host(o), o_w, tol["o"], "o")
-    none = np.isneginf(lse_w)
-    assert np.array_equal(np.isneginf(host(lse)), none)
-    inside(host(lse)[~none], lse_w[~none], tol["lse"][~none], "lse")
+    none, lse = np.isneginf(lse_w), host(stats.lse)
+    assert np.array_equal(np.isneginf(lse), none) and stats.o_low is None
+    inside(lse[~none], lse_w[~none], tol["lse"][~none], "lse")
     again, none = faar.faar_attention_masked_fwd(a, plan, dev(q), kd, vd, want_lse=False)
     assert none is None and torch.equal(again, o)
 
@@ -299,9 +305,9 @@ def test_equal_causal_sequences_are_the_causal_attention():
     plan = faar.faar_attention_plan(a)
     o, lse = faar.faar_attention_masked_fwd(a, plan, q, k, v)
     o2, lse2 = faar.faar_attention_fwd(q, k, v, n_seq, n_q, n_kv)
-    (_, _, *_), tol = c.oracle()
+    (_, _, *_), tol = c.oracle(low=False)
     inside(host(o), host(o2), 2 * tol["o"], "o")           # each within tol of the same value
-    inside(host(lse), host(lse2), 2 * tol["lse"], "lse")
+    inside(host(lse.lse), host(lse2), 2 * tol["lse"], "lse")
     for x, y, n in zip(faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, lse), faar.faar_attention_bwd(d_o, q, k, v, o2, lse2, n_seq, n_q, n_kv),
                        ("dq", "dk", "dv")):
         inside(host(x), host(y), 2 * tol[n], n)
@@ -337,7 +343,7 @@ def test_runs_agree_and_rows_do_not_see_other_sequences():
     plan = faar.faar_attention_plan(a)
     def run(q, k, v, d_o):
         o, lse = faar.faar_attention_masked_fwd(a, plan, q, k, v)
-        return (o, lse, *faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, lse))
+        return (o, lse.lse, lse.o_low, *faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, lse))
     want = run(q, k, v, d_o)
     rows = torch.from_numpy(c.q_rows).cuda()
     part = lambda t: (t if t.shape[0] == c.Tq else t.t())[rows]
@@ -393,7 +399,7 @@ def test_wrong_plans_and_lengths_are_answered_with_nan():
     a, (q, k, v, d_o) = c.device()
     good = faar.faar_attention_plan(a)
     o, lse = faar.faar_attention_masked_fwd(a, good, q, k, v)
-    all_nan = lambda *ts: all(bool(torch.isnan(t.float()).all()) for t in ts)
+    all_nan = lambda *ts: all(bool(torch.isnan((t.lse if isinstance(t, faar.AttentionStats) else t).float()).all()) for t in ts)
     # a plan of another mask
     for change in (dict(window=9), dict(causal=False)):
         other = faar.attention_description(c.n_q, c.n_kv, c.dh, c.Tq, c.Tk, *(ints(t) for t in list(zip(*c.seqs))[:2]), **change)
@@ -458,9 +464,10 @@ def test_refusals():
            (-6, dict(window=-1)), (-6, dict(flags=2)), (-6, dict(scale=0.0)), (-6, dict(scale=float("nan"))), (-6, dict(scale=float("inf"))),
            (-6, dict(cap=-1.0)), (-6, dict(cap=float("inf"))), (-6, dict(cap=1e-45)), (-6, dict(q_start=half)), (-6, dict(prefix=half)), (-6, dict(slopes=half))]
     big = 1 << 40
-    fwd = lambda a, plan=P, pb=big, q=P, k=P, v=P, o=P, lse=P, ws=P, wb=big: L.faar_attention_masked_fwd(a, plan, pb, q, k, v, o, lse, ws, wb, nul)
-    bwd = lambda a, plan=P, pb=big, d_o=P, q=P, k=P, v=P, o=P, lse=P, dq=P, dk=P, dv=P, ws=P, wb=big: \
-        L.faar_attention_masked_bwd(a, plan, pb, d_o, q, k, v, o, lse, dq, dk, dv, ws, wb, nul)
+    fwd = lambda a, plan=P, pb=big, q=P, k=P, v=P, o=P, lse=P, low=nul, ws=P, wb=big: \
+        L.faar_attention_masked_fwd(a, plan, pb, q, k, v, o, lse, low, ws, wb, nul)
+    bwd = lambda a, plan=P, pb=big, d_o=P, q=P, k=P, v=P, o=P, lse=P, low=nul, dq=P, dk=P, dv=P, ws=P, wb=big: \
+        L.faar_attention_masked_bwd(a, plan, pb, d_o, q, k, v, o, lse, low, dq, dk, dv, ws, wb, nul)
     for code, kw in bad:
         a = desc(**kw)
         r = ctypes.byref(a)
@@ -479,6 +486,7 @@ def test_refusals():
     assert L.faar_attention_plan(r, odd, pb, nul) == -6 and L.faar_attention_plan(r, P, pb - 1, nul) == -4
     for name in ("plan", "q", "k", "v", "o"):
         assert fwd(r, **{name: nul}) == -1 and fwd(r, **{name: odd}) == -6, name
+    assert fwd(r, low=odd) == -6 and bwd(r, low=odd) == -6
     assert fwd(r, lse=ctypes.c_void_p(half)) == -6 and fwd(r, ws=nul) == -4 and fwd(r, wb=wf - 1) == -4 and fwd(r, pb=pb - 1) == -4
     for name in ("plan", "d_o", "q", "k", "v", "o", "dq", "dk", "dv"):
         assert bwd(r, **{name: nul}) == -1 and bwd(r, **{name: odd}) == -6, name
@@ -486,4 +494,4 @@ def test_refusals():
     t = desc(q_start=None, q_len=None, k_start=p, k_len=p, Tq=2)
     r = ctypes.byref(t)
     assert L.faar_attention_plan_bytes(r) > 0 and L.faar_attention_masked_workspace_bytes(r, 0) > 4 * 66 * 4
-    assert L.faar_attention_masked_workspace_bytes(r, 1) == 0 and bwd(r) == -7
+    assert L.faar_attention_masked_workspace_bytes(r, 1) == 0 and bwd(r) == -7 and fwd(r, low=P) == -7
