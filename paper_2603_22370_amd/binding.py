@@ -3,6 +3,7 @@ only.  torch is used for device memory and streams; every step of the method run
 kernels behind the C ABI.  There is no fallback: a missing library raises."""
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
@@ -219,21 +220,45 @@ def _dev(*ts):
             raise ValueError("tensors must be contiguous device tensors")
 
 
-def _rows(where, **ts):
-    """Device tensors [rows, width] whose rows may lie further apart than they are wide."""
-    for name, t in ts.items():
-        if t is not None and (not t.is_cuda or t.dim() != 2 or t.dtype != torch.bfloat16 or (t.shape[1] > 1 and t.stride(1) != 1)):
-            raise ValueError(f"{where}: {name} must be a bf16 device tensor [rows, width] with contiguous rows")
+# The calls below are also made for single tokens, where what Python does around a launch counts as much as the kernel: addresses go
+# over as plain integers, and each tensor is looked at once.
+_BF16, _F32 = torch.bfloat16, torch.float32
 
 
-def _ld(t):
-    """Elements between the starts of neighbouring rows (0: absent)."""
-    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _raw_stream(t):
+    """The current stream, as an integer, on the tensor's device, which must be the current one: kernels are launched there."""
+    device = t.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError("the tensors are on another device than the current one")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _row_stride(t, rows, width, where):
+    """Elements between the starts of neighbouring rows of a bf16 device tensor [rows, width], whose rows may lie further apart than they
+    are wide."""
+    if t.dtype is not _BF16 or not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{where}: bf16 device tensors [rows, width] are wanted")
+    if t.shape != (rows, width):
+        raise ValueError(f"{where}: a tensor is {tuple(t.shape)}, not {(rows, width)}")
+    ld, step = t.stride()
+    if step != 1 and width > 1:
+        raise ValueError(f"{where}: the entries of a row must lie side by side")
+    return max(ld, width) if rows == 1 else ld
+
+
+def _whole(t, dtype, numel, where):
+    """A contiguous device tensor of that type and size."""
+    if t.dtype is not dtype or t.numel() != numel or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{where}: a contiguous {dtype} device tensor of {numel} entries is wanted")
 
 
 def _zeros_like_rows(t):
     """Zeros with the shape and the row stride of t."""
-    return torch.zeros((t.shape[0], _ld(t)), dtype=t.dtype, device=t.device)[:, :t.shape[1]]
+    return t.new_zeros((t.shape[0], max(t.stride(0), t.shape[1])))[:, :t.shape[1]]
 
 
 def _check(rc: int, where: str):
@@ -584,15 +609,16 @@ def faar_rope(x, n_heads, cos_t, sin_t, inverse=False, out=None):
 
 
 def faar_layernorm_fwd(x, g, b=None, eps=1e-5):
-    """Layer norm.  -> (h bf16 [T, D], mean f32 [T], rstd f32 [T])."""
-    _dev(x, g, b)
+    """Layer norm.  x [T, D] float32 or bf16; g, b float32 [D].  -> (h bf16 [T, D], mean f32 [T], rstd f32 [T])."""
+    where = "faar_layernorm_fwd"
     T, D = x.shape
-    if any(t is not None and (t.dtype != torch.float32 or t.numel() != D) for t in (g, b)):
-        raise ValueError("faar_layernorm_fwd: g, b float32 [D]")
-    h = torch.empty((T, D), dtype=torch.bfloat16, device=x.device)
-    mean, rstd = torch.empty((2, T), dtype=torch.float32, device=x.device)
-    _check(lib().faar_layernorm_fwd(_ptr(x), _dt(x), T, D, _ptr(g), _ptr(b), float(eps), _ptr(h), _ptr(mean), _ptr(rstd), _stream()),
-           "faar_layernorm_fwd")
+    _whole(x, _BF16 if x.dtype is _BF16 else _F32, T * D, where)
+    _whole(g, _F32, D, where)
+    if b is not None:
+        _whole(b, _F32, D, where)
+    h, mean, rstd = x.new_empty((T, D), dtype=_BF16), x.new_empty(T, dtype=_F32), x.new_empty(T, dtype=_F32)
+    _check(lib().faar_layernorm_fwd(x.data_ptr(), _dt(x), T, D, g.data_ptr(), _at(b), eps, h.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                    _raw_stream(x)), where)
     return h, mean, rstd
 
 
@@ -603,19 +629,23 @@ def layernorm_workspace(T, D, device="cuda"):
 
 def faar_layernorm_bwd(dh1, x, g, mean, rstd, dh2=None, d_res=None, dh3=None, want_dg=False, want_db=False, ws=None):
     """-> (dx bf16 [T, D], dg f32 [D] or None, db f32 [D] or None)."""
-    _dev(dh1, dh2, dh3, x, g, mean, rstd, d_res, ws)
+    where = "faar_layernorm_bwd"
     T, D = x.shape
-    if any(t is not None and (t.dtype != torch.bfloat16 or t.shape != x.shape) for t in (dh1, dh2, dh3, d_res)):
-        raise ValueError("faar_layernorm_bwd: gradients are bf16 [T, D]")
-    if any(t.dtype != torch.float32 or t.numel() != n for t, n in ((g, D), (mean, T), (rstd, T))):
-        raise ValueError("faar_layernorm_bwd: g float32 [D], mean and rstd float32 [T]")
-    dx = torch.empty((T, D), dtype=torch.bfloat16, device=x.device)
-    dg, db = (torch.empty(D, dtype=torch.float32, device=x.device) if w else None for w in (want_dg, want_db))
+    _whole(x, _BF16 if x.dtype is _BF16 else _F32, T * D, where)
+    for t in (dh1, dh2, dh3, d_res):
+        if t is not None:
+            _whole(t, _BF16, T * D, where)
+    _whole(g, _F32, D, where)
+    _whole(mean, _F32, T, where)
+    _whole(rstd, _F32, T, where)
+    dx = x.new_empty((T, D), dtype=_BF16)
+    dg, db = (x.new_empty(D, dtype=_F32) if w else None for w in (want_dg, want_db))
     if ws is None and (want_dg or want_db):
         ws = layernorm_workspace(T, D, device=x.device)
-    _check(lib().faar_layernorm_bwd(_ptr(dh1), _ptr(dh2), _ptr(dh3), _ptr(x), _dt(x), T, D, _ptr(g), _ptr(mean), _ptr(rstd), _ptr(d_res),
-                                    _ptr(dx), _ptr(dg), _ptr(db), _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
-           "faar_layernorm_bwd")
+    _dev(ws)
+    _check(lib().faar_layernorm_bwd(dh1.data_ptr(), _at(dh2), _at(dh3), x.data_ptr(), _dt(x), T, D, g.data_ptr(), mean.data_ptr(),
+                                    rstd.data_ptr(), _at(d_res), dx.data_ptr(), _at(dg), _at(db), _at(ws), 0 if ws is None else ws.numel(),
+                                    _raw_stream(x)), where)
     return dx, dg, db
 
 
@@ -626,20 +656,26 @@ def faar_rope_axes(q, k, n_q, n_k, dh, pos, axis, freq, pairs=False, inverse=Fal
     """Rotary embedding over several position axes.  q bf16 [T, n_q * dh], k bf16 [T, n_k * dh] or None (rows may lie apart: slices of a
     fused projection); pos int32 [n_axes, T]; axis, freq: sequences of the position axis and the frequency (radians per position) of each
     rotated pair, len(freq) = rot / 2.  out: (yq, yk), which may be q and k.  -> (yq, yk)."""
-    yq, yk = (torch.empty((q.shape[0], q.shape[1]), dtype=q.dtype, device=q.device),
-              None if k is None else torch.empty((k.shape[0], k.shape[1]), dtype=k.dtype, device=k.device)) if out is None else out
-    _rows("faar_rope_axes", q=q, k=k, yq=yq, yk=yk)
-    _dev(pos)
+    where = "faar_rope_axes"
     T, half = q.shape[0], len(freq)
-    if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != T or len(axis) != half:
+    if len(axis) != half or pos.dim() != 2:
         raise ValueError("faar_rope_axes: pos int32 [n_axes, T], one axis for each frequency")
-    if q.shape[1] != n_q * dh or yq.shape != q.shape or (k is None) != (yk is None) or \
-            (k is not None and (k.shape != (T, n_k * dh) or yk.shape != k.shape)):
-        raise ValueError("faar_rope_axes: q [T, n_q * dh], k [T, n_k * dh], outputs alike")
-    ax, fr = (ctypes.c_uint8 * max(half, 1))(*axis), (ctypes.c_double * max(half, 1))(*freq)
-    _check(lib().faar_rope_axes(_ptr(q), _ld(q), n_q, _ptr(k), _ld(k), n_k, T, dh, 2 * half, _ptr(pos), pos.shape[0], ax, fr,
-                                (FAAR_ROPE_PAIRS if pairs else 0) | (FAAR_ROPE_INVERSE if inverse else 0), _ptr(yq), _ld(yq), _ptr(yk),
-                                _ld(yk), _stream()), "faar_rope_axes")
+    n_axes = pos.shape[0]
+    _whole(pos, torch.int32, n_axes * T, where)
+    ldq = _row_stride(q, T, n_q * dh, where)
+    ldk = 0 if k is None else _row_stride(k, T, n_k * dh, where)
+    if out is None:
+        yq, yk = q.new_empty((T, n_q * dh)), None if k is None else k.new_empty((T, n_k * dh))
+        ldyq, ldyk = n_q * dh, n_k * dh
+    else:
+        yq, yk = out
+        if (k is None) != (yk is None):
+            raise ValueError("faar_rope_axes: k and its output come together")
+        ldyq, ldyk = _row_stride(yq, T, n_q * dh, where), 0 if k is None else _row_stride(yk, T, n_k * dh, where)
+    fr = array.array("d", freq)
+    _check(lib().faar_rope_axes(q.data_ptr(), ldq, n_q, _at(k), ldk, n_k, T, dh, 2 * half, pos.data_ptr(), n_axes, bytes(list(axis)),
+                                fr.buffer_info()[0], (FAAR_ROPE_PAIRS if pairs else 0) | (FAAR_ROPE_INVERSE if inverse else 0), yq.data_ptr(),
+                                ldyq, _at(yk), ldyk, _raw_stream(q)), where)
     return yq, yk
 
 
@@ -732,52 +768,52 @@ class AttentionStats:
         self.lse, self.o_low = lse, o_low
 
 
-def _masked_rows(a, where, q, k, v, o, stats):
-    _rows(where, q=q, k=k, v=v, o=o)
-    kv = (a.Tk, a.n_kv * a.dh)
-    if q.shape != (a.Tq, a.n_q * a.dh) or o.shape != q.shape or k.shape != kv or v.shape != kv:
-        raise ValueError(f"{where}: q, o [Tq, n_q * dh]; k, v [Tk, n_kv * dh]")
+def _masked_call(a, where, plan, q, k, v, o, stats, ws):
+    """The description with the row strides of a call's tensors (a copy: the caller's may be in use by another thread)."""
+    Tq, Tk, qd, kd = a.Tq, a.Tk, a.n_q * a.dh, a.n_kv * a.dh
+    d = faar_attention.from_buffer_copy(a)
+    d.ldq, d.ldk, d.ldv, d.ldo = (_row_stride(q, Tq, qd, where), _row_stride(k, Tk, kd, where), _row_stride(v, Tk, kd, where),
+                                  _row_stride(o, Tq, qd, where))
     if stats is not None:
-        _dev(stats.lse, stats.o_low)
-        if stats.lse.dtype != torch.float32 or stats.lse.numel() != a.n_q * a.Tq or \
-                (stats.o_low is not None and (stats.o_low.dtype != torch.int8 or stats.o_low.shape != q.shape)):
-            raise ValueError(f"{where}: lse float32 [n_q, Tq], o_low int8 [Tq, n_q * dh]")
-    d = faar_attention.from_buffer_copy(a)               # the caller's description may be in use by another thread
-    d.ldq, d.ldk, d.ldv, d.ldo = _ld(q), _ld(k), _ld(v), _ld(o)
+        _whole(stats.lse, _F32, a.n_q * Tq, where)
+        if stats.o_low is not None:
+            _whole(stats.o_low, torch.int8, Tq * qd, where)
+    _dev(plan, ws)
     return d
 
 
 def faar_attention_masked_fwd(a, plan, q, k, v, out=None, want_lse=True, ws=None):
     """-> (o bf16 [Tq, n_q * dh], stats for the backward (stats.lse float32 [n_q, Tq]), or None without want_lse).  Rows of no sequence
     keep what out holds (0 where out is not given)."""
-    o = torch.zeros((a.Tq, a.n_q * a.dh), dtype=torch.bfloat16, device=q.device) if out is None else out
+    where = "faar_attention_masked_fwd"
+    o = q.new_zeros((a.Tq, a.n_q * a.dh)) if out is None else out
     stats = None
     if want_lse:
-        single = a.q_len is None
-        stats = AttentionStats(torch.empty((a.n_q, a.Tq), dtype=torch.float32, device=q.device),
-                               None if single else torch.empty((a.Tq, a.n_q * a.dh), dtype=torch.int8, device=q.device))
-    d = _masked_rows(a, "faar_attention_masked_fwd", q, k, v, o, stats)
-    ws = attention_masked_workspace(a) if ws is None else ws
-    _dev(plan, ws)
-    _check(lib().faar_attention_masked_fwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
-                                           _ptr(stats.lse) if stats else None, _ptr(stats.o_low) if stats else None, _ptr(ws), ws.numel(),
-                                           _stream()), "faar_attention_masked_fwd")
+        stats = AttentionStats(q.new_empty((a.n_q, a.Tq), dtype=_F32),
+                               None if a.q_len is None else q.new_empty((a.Tq, a.n_q * a.dh), dtype=torch.int8))
+    if ws is None:
+        ws = attention_masked_workspace(a)
+    d = _masked_call(a, where, plan, q, k, v, o, stats, ws)
+    _check(lib().faar_attention_masked_fwd(d, plan.data_ptr(), plan.numel(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                                           _at(stats.lse) if stats else None, _at(stats.o_low) if stats else None, ws.data_ptr(), ws.numel(),
+                                           _raw_stream(q)), where)
     return o, stats
 
 
 def faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, out=None, ws=None):
     """-> (dq, dk, dv) bf16, shaped like q, k, v (out: the same three, with the row strides of q, k and v).  Rows of no sequence keep what
     out holds (0 where out is not given)."""
+    where = "faar_attention_masked_bwd"
     dq, dk, dv = tuple(_zeros_like_rows(t) for t in (q, k, v)) if out is None else out
-    d = _masked_rows(a, "faar_attention_masked_bwd", q, k, v, o, stats)
-    _rows("faar_attention_masked_bwd", d_o=d_o, dq=dq, dk=dk, dv=dv)
-    if any(x.shape != y.shape or _ld(x) != _ld(y) for x, y in ((d_o, o), (dq, q), (dk, k), (dv, v))):
-        raise ValueError("faar_attention_masked_bwd: gradients have the shapes and row strides of what they belong to")
-    ws = attention_masked_workspace(a, backward=True) if ws is None else ws
-    _dev(plan, ws)
-    _check(lib().faar_attention_masked_bwd(ctypes.byref(d), _ptr(plan), plan.numel(), _ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
-                                           _ptr(stats.lse), _ptr(stats.o_low), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()),
-           "faar_attention_masked_bwd")
+    if ws is None:
+        ws = attention_masked_workspace(a, backward=True)
+    d = _masked_call(a, where, plan, q, k, v, o, stats, ws)
+    for x, y, ld in ((d_o, o, d.ldo), (dq, q, d.ldq), (dk, k, d.ldk), (dv, v, d.ldv)):
+        if _row_stride(x, *y.shape, where) != ld:
+            raise ValueError(f"{where}: a gradient has another row stride than what it belongs to")
+    _check(lib().faar_attention_masked_bwd(d, plan.data_ptr(), plan.numel(), d_o.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                           o.data_ptr(), stats.lse.data_ptr(), _at(stats.o_low), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                           ws.data_ptr(), ws.numel(), _raw_stream(q)), where)
     return dq, dk, dv
 
 
