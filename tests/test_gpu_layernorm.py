@@ -17,7 +17,7 @@ from paper_2603_22370_amd import binding as fb
 
 U8 = 2.0 ** -8
 SHAPES = [(1, 8), (1, 2048), (7, 40), (67, 64), (33, 136), (300, 256), (5, 520), (65, 1032), (130, 2048), (9, 2056), (3, 6152), (2, 16384),
-          (2500, 96)]
+          (2500, 96), (2100, 512), (300, 16384), (6200, 520), (700, 4104)]
 
 
 def dev(a, bf16=True):
