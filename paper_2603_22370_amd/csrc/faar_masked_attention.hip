@@ -287,10 +287,23 @@ __device__ __forceinline__ void masked_block(MaskedState<DH>& st, uint32_t k_lds
   f32x16 s[NT];            // rows = keys, column = query
 #pragma unroll
   for (int kt = 0; kt < NT; ++kt) s[kt] = zero16();
+  // Operands from LDS are requested kRing - 1 matrix instructions ahead, and the first of V's before the exponents, during which they
+  // arrive; scheduling barriers keep the order.
+  constexpr int kRing = 6, kFirst = 4, kQK = NT * KS, kPV = NT * 2 * DT;
+  bf16x8 f[kRing];
+  auto fetch_k = [&](int i) { f[i % kRing] = Tl::rows(k_lds + ra, h0 + i % NT, i / NT); };
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
+  for (int i = 0; i < kRing - 1 && i < kQK; ++i) fetch_k(i);
 #pragma unroll
-    for (int kt = 0; kt < NT; ++kt) s[kt] = mfma(Tl::rows(k_lds + ra, h0 + kt, ks), st.qf[ks], s[kt]);
+  for (int i = 0; i < kQK; ++i) {
+    if (i + kRing - 1 < kQK) fetch_k(i + kRing - 1);
+    s[i % NT] = mfma(f[i % kRing], st.qf[i / NT], s[i % NT]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  auto fetch_v = [&](int i) { f[i % kRing] = Tl::cols(v_lds + ca, h0 + i / (2 * DT), i / DT % 2, i % DT); };
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) fetch_v(i);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int kt = 0; kt < NT; ++kt)
 #pragma unroll
@@ -342,17 +355,22 @@ __device__ __forceinline__ void masked_block(MaskedState<DH>& st, uint32_t k_lds
       ps += p;
     }
   st.l += ps;
+  Frag p[NT][2];
 #pragma unroll
   for (int kt = 0; kt < NT; ++kt) {
-    Frag p0, p1;
-    p0.v = pack8<0>(s[kt]);
-    p1.v = pack8<1>(s[kt]);
+    p[kt][0].v = pack8<0>(s[kt]);
+    p[kt][1].v = pack8<1>(s[kt]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) st.lr = add_pair(p1.w[i], add_pair(p0.w[i], st.lr));
+    for (int i = 0; i < 4; ++i) st.lr = add_pair(p[kt][1].w[i], add_pair(p[kt][0].w[i], st.lr));
+  }
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 0, dt), p0.v, st.oacc[dt]);
+  for (int i = kFirst; i < kRing - 1 && i < kPV; ++i) fetch_v(i);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) st.oacc[dt] = mfma(Tl::cols(v_lds + ca, h0 + kt, 1, dt), p1.v, st.oacc[dt]);
+  for (int i = 0; i < kPV; ++i) {
+    if (i + kRing - 1 < kPV) fetch_v(i + kRing - 1);
+    st.oacc[i % DT] = mfma(f[i % kRing], p[i / (2 * DT)][i / DT % 2].v, st.oacc[i % DT]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -367,6 +385,32 @@ __device__ __forceinline__ uint32_t low_bytes(const float (&x)[4], const uint2& 
   }
   return r;
 }
+// A wavefront's 32 rows x DH results, which lie across its lanes (lane n, half hi: row n, columns 32 dt + 8 j + 4 hi + 0..3), go through LDS
+// and leave as 16 bytes a lane, a row after the other: stored as they lie, 8 bytes of 32 rows an instruction, they would take more time
+// than all else that a short sequence costs (8192 rows of 16 heads of 128: 23 us of 53, see below).  Rows are padded by 16 bytes.
+template <int DH>
+struct RowStage {
+  static constexpr int PITCH = DH * 2 + 16, LOW_PITCH = DH + 16, BYTES = 32 * (PITCH + LOW_PITCH);
+  static __device__ __forceinline__ void put(char* at, int lane, int dt, int j, const float (&x)[4], bool low) {
+    const int n = lane & 31, col = 32 * dt + 8 * j + 4 * (lane >> 5);
+    const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    *reinterpret_cast<uint2*>(at + n * PITCH + col * 2) = w;
+    if (low) *reinterpret_cast<uint32_t*>(at + 32 * PITCH + n * LOW_PITCH + col) = low_bytes(x, w);
+  }
+  // rows rows (of 32) and dh columns to out, `ld` elements apart, and the low bytes to out_low, ld_low apart
+  static __device__ __forceinline__ void flush(const char* at, int lane, int rows, int dh, bf16_t* out, int64_t ld, uint8_t* out_low, int64_t ld_low) {
+    constexpr int CPR = DH / 8, RPP = 64 / CPR;        // chunks per row, rows per pass
+    const int chunk = lane % CPR;
+#pragma unroll
+    for (int i = 0; i < 32 / RPP; ++i) {
+      const int row = i * RPP + lane / CPR;
+      if (row >= rows || chunk * 8 >= dh) continue;
+      *reinterpret_cast<uint4*>(out + row * ld + chunk * 8) = *reinterpret_cast<const uint4*>(at + row * PITCH + chunk * 16);
+      if (out_low) *reinterpret_cast<uint2*>(out_low + row * ld_low + chunk * 8) = *reinterpret_cast<const uint2*>(at + 32 * PITCH + row * LOW_PITCH + chunk * 8);
+    }
+  }
+};
+
 // the float of a bf16 and its byte
 __device__ __forceinline__ float with_low(uint32_t bf16_top, uint32_t byte) {
   return __uint_as_float(bf16_top + (static_cast<uint32_t>(static_cast<int>(byte << 24) >> 24) << 8));
@@ -428,24 +472,24 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
     masked_block<DH, kMode, 2>(st, k_lds, v_lds, ra, ca, sc, 0, !(k0 >= sb.lo && k0 + kTok <= sa.hi), k0 + 4 * hi - seen.lo,
                                max(0, seen.hi - seen.lo), gap);
   }
-  if (!live) return;
-  const int64_t t = (int64_t)row0 + 32 * wave + (again(lane) & 31);
+  __syncthreads();                                     // the tiles have been read: their place is free
+  if (mine <= 0) return;
   const float lt = half_sum(st.l), lr = half_sum(st.lr);
   const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;      // a query that sees no key: 0
+  char* stage = reinterpret_cast<char*>(lds) + wave * RowStage<DH>::BYTES;
+  static_assert(4 * RowStage<DH>::BYTES <= sizeof(lds), "rows fit in the stages");
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (dt * 32 + 8 * j < d.dh) {
-        const int c = head * d.dh + dt * 32 + 8 * j + 4 * hi;
-        float x[4];
+    for (int j = 0; j < 4; ++j) {
+      float x[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = st.oacc[dt][4 * j + r] * inv;
-        const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-        *reinterpret_cast<uint2*>(O + t * d.ldo + c) = w;
-        if (o_low) *reinterpret_cast<uint32_t*>(o_low + t * ((int64_t)d.n_q * d.dh) + c) = low_bytes(x, w);
-      }
-  if (lse && hi == 0) lse[(int64_t)head * d.Tq + t] = lt > 0.0f ? st.mc * kLn2 + logf(lt) : -INFINITY;
+      for (int r = 0; r < 4; ++r) x[r] = st.oacc[dt][4 * j + r] * inv;
+      RowStage<DH>::put(stage, lane, dt, j, x, o_low != nullptr);
+    }
+  const int64_t t = (int64_t)row0 + 32 * wave, width = (int64_t)d.n_q * d.dh;
+  if (lse && hi == 0 && n < mine) lse[(int64_t)head * d.Tq + t + n] = lt > 0.0f ? st.mc * kLn2 + logf(lt) : -INFINITY;
+  RowStage<DH>::flush(stage, lane, mine, d.dh, O + t * d.ldo + head * d.dh, d.ldo, o_low ? o_low + t * width + head * d.dh : nullptr, width);
 }
 
 // ---- backward: dq ---------------------------------------------------------------------------------------------------------------
@@ -589,15 +633,19 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
                                       gap - 32 * kt);
     }
   }
-  if (!live) return;
-  const int64_t t = (int64_t)row0 + 32 * wave + (again(lane) & 31);
+  __syncthreads();
+  if (mine <= 0) return;
+  char* stage = reinterpret_cast<char*>(lds) + wave * RowStage<DH>::BYTES;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (dt * 32 + 8 * j < d.dh)
-        store4_bf16(dQ + t * d.ldq + head * d.dh + dt * 32 + 8 * j + 4 * hi, acc[dt][4 * j] * d.scale, acc[dt][4 * j + 1] * d.scale,
-                    acc[dt][4 * j + 2] * d.scale, acc[dt][4 * j + 3] * d.scale);
+    for (int j = 0; j < 4; ++j) {
+      float x[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = acc[dt][4 * j + r] * d.scale;
+      RowStage<DH>::put(stage, lane, dt, j, x, false);
+    }
+  RowStage<DH>::flush(stage, lane, mine, d.dh, dQ + ((int64_t)row0 + 32 * wave) * d.ldq + head * d.dh, d.ldq, nullptr, 0);
 }
 
 // ---- backward: dk, dv -----------------------------------------------------------------------------------------------------------
@@ -754,20 +802,26 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
     give[dt * 64] = g;
   }
   __syncthreads();
-  if (!live) return;
-  const int64_t t = (int64_t)row0 + 32 * kw + (again(lane) & 31);
+  f32x16 sum[DT];
   const float k = qw == 0 ? d.scale : 1.0f;
-  bf16_t* out = qw == 0 ? dK + t * d.ldk : dV + t * d.ldv;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
-    f32x16 r = take[dt * 64];
+    const f32x16 r = take[dt * 64];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = (qw == 0 ? dk[dt][i] : dv[dt][i]) + r[i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (dt * 32 + 8 * i < d.dh)
-        store4_bf16(out + kvh * d.dh + dt * 32 + 8 * i + 4 * hi, r[4 * i] * k, r[4 * i + 1] * k, r[4 * i + 2] * k, r[4 * i + 3] * k);
+    for (int i = 0; i < 16; ++i) sum[dt][i] = ((qw == 0 ? dk[dt][i] : dv[dt][i]) + r[i]) * k;
   }
+  __syncthreads();                                     // all has been taken: the place is free
+  if (mine <= 0) return;
+  char* stage = reinterpret_cast<char*>(lds) + wave * RowStage<DH>::BYTES;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x[4] = {sum[dt][4 * i], sum[dt][4 * i + 1], sum[dt][4 * i + 2], sum[dt][4 * i + 3]};
+      RowStage<DH>::put(stage, lane, dt, i, x, false);
+    }
+  const int64_t t = (int64_t)row0 + 32 * kw, ld = qw == 0 ? d.ldk : d.ldv;
+  RowStage<DH>::flush(stage, lane, mine, d.dh, (qw == 0 ? dK : dV) + t * ld + kvh * d.dh, ld, nullptr, 0);
 }
 
 // ---- one token a sequence ---------------------------------------------------------------------------------------------------------
