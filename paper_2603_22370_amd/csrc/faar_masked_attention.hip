@@ -44,13 +44,21 @@ __device__ __attribute__((aligned(16))) const uint32_t kZeroChunk[4] = {0, 0, 0,
 __device__ __forceinline__ void dma16_from(const void* gptr, uint32_t lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory", "m0");
 }
-// 64 rows of a tile of which `valid` are there and dh of its columns: whole tiles by the copies that need no comparison; what is
-// missing is filled with zeros (a masked probability of 0 times whatever lies behind a sequence would not be 0 for all values)
+// What a head's width asks of the tiles: DH entries a row in LDS, KS steps of 16 in products over dh, DT blocks of 32 in products that give dh
+struct Heads64 { static constexpr int DH = 64, KS = 4, DT = 2; };
+struct Heads96 { static constexpr int DH = 128, KS = 6, DT = 3; };    // a row as of 128, of which the last quarter is never touched
+struct Heads128 { static constexpr int DH = 128, KS = 8, DT = 4; };
+
+// 64 rows of a tile of which `valid` are there, dh columns of each.  Columns beyond dh are left alone (clear_columns); rows that are
+// missing are filled with zeros (a masked probability of 0 times whatever lies behind a sequence would not be 0 for all values).
 template <int DH>
 __device__ __forceinline__ void copy_tile(const bf16_t* __restrict__ src, int64_t row0, int valid, int64_t ld, int64_t col0, int dh,
                                           uint32_t lane_offset, uint32_t tile, int wave, int tid) {
   typedef Tile<DH> Tl;
-  if (valid >= kTok && dh == DH) {
+  asm volatile("" : "+v"(tid));        // addresses are formed here, where few blocks come by, and not kept in registers throughout
+  const int r = tid / Tl::CPR, col = ((tid % Tl::CPR) ^ Tl::key(r)) * 8;
+  if (col >= dh) return;               // these lanes copy nothing
+  if (valid >= kTok) {
     // addresses that are the same for all lanes go in scalar registers, said lane by lane where the compiler does not see it
 #pragma unroll
     for (int j = 0; j < Tl::COPIES; ++j) {
@@ -60,14 +68,23 @@ __device__ __forceinline__ void copy_tile(const bf16_t* __restrict__ src, int64_
     }
     return;
   }
-  asm volatile("" : "+v"(tid));        // addresses are formed here, where few blocks come by, and not kept in registers throughout
-  const int r = tid / Tl::CPR, col = ((tid % Tl::CPR) ^ Tl::key(r)) * 8;
 #pragma unroll
   for (int j = 0; j < Tl::COPIES; ++j) {
     const int row = r + j * (256 / Tl::CPR);
-    const void* p = row < valid && col < dh ? static_cast<const void*>(src + (row0 + row) * ld + col0 + col) : kZeroChunk;
+    const void* p = row < valid ? static_cast<const void*>(src + (row0 + row) * ld + col0 + col) : kZeroChunk;
     dma16_from(p, __builtin_amdgcn_readfirstlane(tile + 4096u * j + 1024u * wave));
   }
+}
+// zeros in the columns from dh on that the products read, of `tiles` tiles: once a workgroup, since no copy touches them
+template <class H>
+__device__ __forceinline__ void clear_columns(bf16_t* tile, int tiles, int dh, int tid) {
+  typedef Tile<H::DH> Tl;
+  if (dh >= 16 * H::KS) return;
+  const int r = tid / Tl::CPR, c = tid % Tl::CPR, col = (c ^ Tl::key(r)) * 8;
+  if (col < dh || col >= 16 * H::KS) return;
+  for (int i = 0; i < tiles; ++i)
+    for (int j = 0; j < Tl::COPIES; ++j)
+      *reinterpret_cast<uint4*>(tile + i * Tl::ELEMS + (r + j * (256 / Tl::CPR)) * H::DH + c * 8) = make_uint4(0, 0, 0, 0);
 }
 
 struct Seen { int lo, hi; };           // keys [lo, hi) of the sequence; hi <= lo: none
@@ -230,16 +247,22 @@ __device__ __forceinline__ int again(int x) {
   return x;
 }
 
-// a word of the plan, the same for all lanes
-__device__ __forceinline__ int word(const int* p) { return __builtin_amdgcn_readfirstlane(*p); }
-
-// Is this the plan of the call's description?  Every workgroup looks (uniform loads); what is not is answered with NaN.
-__device__ __forceinline__ bool plan_is(const int* __restrict__ plan, const PlanTag& tag, bool backward) {
-  bool ok = word(plan + kPlanBad) == 0 && !(backward && word(plan + kPlanNoBackward) != 0);
+// A workgroup's look at the plan: one load brings the header (lanes 0 .. 15) and the words of its item (16 .. 23), which lie inside the
+// plan's memory whether or not that many items are in use
+struct PlanWords {
+  int w;
+  __device__ __forceinline__ PlanWords(const int* __restrict__ plan, int items_at, int item, int lane)
+      : w(plan[lane < 16 ? lane : items_at + 8 * item + (lane & 7)]) {}
+  __device__ __forceinline__ int header(int i) const { return __builtin_amdgcn_readlane(w, i); }
+  __device__ __forceinline__ int item(int i) const { return __builtin_amdgcn_readlane(w, 16 + i); }
+  // Is this the plan of the call's description?  What is not is answered with NaN.
+  __device__ __forceinline__ bool is(const PlanTag& tag, bool backward) const {
+    bool ok = header(kPlanBad) == 0 && !(backward && header(kPlanNoBackward) != 0);
 #pragma unroll
-  for (int i = 0; i < kPlanTagWords; ++i) ok = ok && word(plan + i) == tag.w[i];
-  return ok;
-}
+    for (int i = 0; i < kPlanTagWords; ++i) ok = ok && header(i) == tag.w[i];
+    return ok;
+  }
+};
 __device__ __forceinline__ void fill_nan(bf16_t* p, int64_t rows, int64_t width, int64_t ld) {
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
     for (int64_t c = threadIdx.x; c < width; c += blockDim.x) p[r * ld + c] = 0x7FC0;
@@ -264,10 +287,10 @@ __device__ __forceinline__ float cap_half(const Scores& sc, float x) {
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------------------------
-template <int DH>
+template <class H>
 struct MaskedState {
-  bf16x8 qf[DH / 16];
-  f32x16 oacc[DH / 32];   // rows = dh, column = query lane % 32
+  bf16x8 qf[H::KS];
+  f32x16 oacc[H::DT];   // rows = dh, column = query lane % 32
   float mc, l, lr;        // reference maximum (units of log 2), this half-wave's share of the denominator, and that of rounded probabilities
 };
 
@@ -279,10 +302,10 @@ __device__ __forceinline__ float add_pair(uint32_t w, float a) {
 
 // NT x 32 keys of tiles at k_lds, v_lds (first 32: half `h0`).  first: index of the lane's first key relative to what is compared:
 // `len` keys from 0 on are seen (masked); gap: distance of the lane's first key from its query.
-template <int DH, int kMode, int NT>
-__device__ __forceinline__ void masked_block(MaskedState<DH>& st, uint32_t k_lds, uint32_t v_lds, uint32_t ra, uint32_t ca, const Scores& sc,
+template <class H, int kMode, int NT>
+__device__ __forceinline__ void masked_block(MaskedState<H>& st, uint32_t k_lds, uint32_t v_lds, uint32_t ra, uint32_t ca, const Scores& sc,
                                              int h0, bool masked, int first, int len, float gap) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   f32x16 s[NT];            // rows = keys, column = query
 #pragma unroll
@@ -416,22 +439,22 @@ __device__ __forceinline__ float with_low(uint32_t bf16_top, uint32_t byte) {
   return __uint_as_float(bf16_top + (static_cast<uint32_t>(static_cast<int>(byte << 24) >> 24) << 8));
 }
 
-template <int DH, int kMode>
+template <class H, int kMode>
 __global__ void __launch_bounds__(256, 2)
 k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
              PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse, uint8_t* __restrict__ o_low) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
-  if (!plan_is(plan, tag, false)) {
+  const int item = blockIdx.x / d.n_q, pair = blockIdx.x % d.n_q;
+  const PlanWords w(plan, z.q_at, item, threadIdx.x & 63);
+  if (!w.is(tag, false)) {
     fill_nan(O, d.Tq, (int64_t)d.n_q * d.dh, d.ldo);
     if (lse) fill_nan(lse, d.Tq * d.n_q);
     return;
   }
-  const int item = blockIdx.x / d.n_q, pair = blockIdx.x % d.n_q;
-  if (item >= word(plan + kPlanQItems)) return;
-  const int* w = plan + z.q_at + 8 * item;
-  const int row0 = word(w + 0), rows = word(w + 1), pos0 = word(w + 2), k_start = word(w + 3), k_len = word(w + 4), prefix = word(w + 5), kb0 = word(w + 6), kb1 = word(w + 7);
+  if (item >= w.header(kPlanQItems)) return;
+  const int row0 = w.item(0), rows = w.item(1), pos0 = w.item(2), k_start = w.item(3), k_len = w.item(4), prefix = w.item(5), kb0 = w.item(6), kb1 = w.item(7);
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
@@ -444,7 +467,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
   const Seen seen = live ? keys_of(p, k_len, prefix, window, causal) : Seen{0, 0};
   const Seen sa = keys_of(pos0 + 32 * wave, k_len, prefix, window, causal), sb = keys_of(pos0 + 32 * wave + mine - 1, k_len, prefix, window, causal);
 
-  MaskedState<DH> st;
+  MaskedState<H> st;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
     st.qf[ks] = live && ks * 16 + 8 * hi < d.dh ? load_frag16(Q + ((int64_t)row0 + 32 * wave + n) * d.ldq + head * d.dh + ks * 16 + 8 * hi) : bf16x8{};
@@ -460,6 +483,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
     copy_tile<DH>(K, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
     copy_tile<DH>(V, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldv, kvcol, d.dh, from_v, at + Tl::ELEMS * 2, wave, tid);
   };
+  clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
   if (kb0 < kb1) request(kb0);
   for (int kb = kb0; kb < kb1; ++kb) {
     FAAR_WAIT_VMCNT(0);                                // block kb has landed (mine); the barrier: everybody's, and nobody reads
@@ -469,7 +493,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
     const int k0 = kb * kTok;
     if (mine <= 0 || k0 >= sb.hi || k0 + kTok <= sa.lo) continue;
     const float gap = static_cast<float>(p - k0 - 4 * hi);
-    masked_block<DH, kMode, 2>(st, k_lds, v_lds, ra, ca, sc, 0, !(k0 >= sb.lo && k0 + kTok <= sa.hi), k0 + 4 * hi - seen.lo,
+    masked_block<H, kMode, 2>(st, k_lds, v_lds, ra, ca, sc, 0, !(k0 >= sb.lo && k0 + kTok <= sa.hi), k0 + 4 * hi - seen.lo,
                                max(0, seen.hi - seen.lo), gap);
   }
   __syncthreads();                                     // the tiles have been read: their place is free
@@ -510,11 +534,11 @@ __device__ __forceinline__ float prob_of(float x, const Scores& sc, float lse2, 
 
 // 32 keys (half kt of the tiles).  The operands from LDS pass through a ring of kRing, each requested kRing - 1 matrix instructions
 // ahead, as in the dk / dv kernel, and for its reason: with all of them requested at once registers run out.
-template <int DH, bool kCap, bool kBias>
-__device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[DH / 32], const bf16x8 (&qf)[DH / 16], const bf16x8 (&dof)[DH / 16], float lse2,
+template <class H, bool kCap, bool kBias>
+__device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x8 (&qf)[H::KS], const bf16x8 (&dof)[H::KS], float lse2,
                                                float dl, uint32_t k_rows, uint32_t v_rows, uint32_t k_cols, const Scores& sc, bool masked,
                                                int first, int len, float gap) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   constexpr int kRing = 4;
   bf16x8 f[kRing];
@@ -554,22 +578,22 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[DH / 32], const bf1
   }
 }
 
-template <int DH, bool kCap, bool kBias>
+template <class H, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                 const bf16_t* __restrict__ O, const uint8_t* __restrict__ o_low, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
                 float* __restrict__ delta, bf16_t* __restrict__ dQ) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
-  if (!plan_is(plan, tag, true)) {
+  const int item = blockIdx.x / d.n_q, pair = blockIdx.x % d.n_q;
+  const PlanWords w(plan, z.q_at, item, threadIdx.x & 63);
+  if (!w.is(tag, true)) {
     fill_nan(dQ, d.Tq, (int64_t)d.n_q * d.dh, d.ldq);
     return;
   }
-  const int item = blockIdx.x / d.n_q, pair = blockIdx.x % d.n_q;
-  if (item >= word(plan + kPlanQItems)) return;
-  const int* w = plan + z.q_at + 8 * item;
-  const int row0 = word(w + 0), rows = word(w + 1), pos0 = word(w + 2), k_start = word(w + 3), k_len = word(w + 4), prefix = word(w + 5), kb0 = word(w + 6), kb1 = word(w + 7);
+  if (item >= w.header(kPlanQItems)) return;
+  const int row0 = w.item(0), rows = w.item(1), pos0 = w.item(2), k_start = w.item(3), k_len = w.item(4), prefix = w.item(5), kb0 = w.item(6), kb1 = w.item(7);
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
@@ -615,6 +639,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
     copy_tile<DH>(K, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
     copy_tile<DH>(V, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldv, kvcol, d.dh, from_v, at + Tl::ELEMS * 2, wave, tid);
   };
+  clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
   if (kb0 < kb1) request(kb0);
   for (int kb = kb0; kb < kb1; ++kb) {
     FAAR_WAIT_VMCNT(0);
@@ -629,7 +654,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
 #pragma unroll 1
     for (int kt = 0; kt < 2; ++kt) {
       const uint32_t half = kt * (32 * DH * 2);
-      masked_dq_tile<DH, kCap, kBias>(acc, qf, dof, lse2, dl, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
+      masked_dq_tile<H, kCap, kBias>(acc, qf, dof, lse2, dl, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
                                       gap - 32 * kt);
     }
   }
@@ -651,11 +676,11 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
 // ---- backward: dk, dv -----------------------------------------------------------------------------------------------------------
 // 32 queries x 32 keys; registers and rings as in the causal kernel.  first: index of the lane's first query relative to the first that
 // sees the lane's key, of `len`; gap: distance of the lane's key from the lane's first query.
-template <int DH, bool kCap, bool kBias>
-__device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[DH / 32], f32x16 (&dv)[DH / 32], const bf16x8 (&kf)[DH / 16],
-                                                const bf16x8 (&vf)[DH / 16], const float* lse_lds, const float* delta_lds, uint32_t q_rows,
+template <class H, bool kCap, bool kBias>
+__device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv)[H::DT], const bf16x8 (&kf)[H::KS],
+                                                const bf16x8 (&vf)[H::KS], const float* lse_lds, const float* delta_lds, uint32_t q_rows,
                                                 uint32_t q_cols, const Scores& sc, bool masked, int first, int len, float gap, int lane) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   constexpr uint32_t kDo = Tile<DH>::ELEMS * 2;     // the dO tile follows the q tile
   typedef Tile<DH> Tl;
   constexpr int kRing = 3;
@@ -712,24 +737,24 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[DH / 32], f32x16 (&
 
 // 64 keys of a key / value head a workgroup: wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
 // block of 64 and 2, 3 the others, and the two sums of a block of keys meet through LDS at the end
-template <int DH, bool kCap, bool kBias>
+template <class H, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                  const float* __restrict__ lse, const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
                  bf16_t* __restrict__ dK, bf16_t* __restrict__ dV) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][q, dO]
   __shared__ __attribute__((aligned(16))) float stats[2][2][kTok];         // [stage][lse, delta]
-  if (!plan_is(plan, tag, true)) {
+  const int item = blockIdx.x / d.n_kv, kvh = blockIdx.x % d.n_kv;
+  const PlanWords w(plan, z.k_at, item, threadIdx.x & 63);
+  if (!w.is(tag, true)) {
     fill_nan(dK, d.Tk, (int64_t)d.n_kv * d.dh, d.ldk);
     fill_nan(dV, d.Tk, (int64_t)d.n_kv * d.dh, d.ldv);
     return;
   }
-  const int item = blockIdx.x / d.n_kv, kvh = blockIdx.x % d.n_kv;
-  if (item >= word(plan + kPlanKItems)) return;
-  const int* w = plan + z.k_at + 8 * item;
-  const int row0 = word(w + 0), rows = word(w + 1), k0 = word(w + 2), q_start = word(w + 3), q_len = word(w + 4), off = word(w + 5), prefix = word(w + 6);
+  if (item >= w.header(kPlanKItems)) return;
+  const int row0 = w.item(0), rows = w.item(1), k0 = w.item(2), q_start = w.item(3), q_len = w.item(4), off = w.item(5), prefix = w.item(6);
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
@@ -769,6 +794,7 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
            __builtin_amdgcn_readfirstlane(lds_addr_of(stats[stage][wave])));
   };
   int head = kvh * rep, blk = first;
+  clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
   if (steps > 0) request(0, head, blk);
   for (int it = 0; it < steps; ++it) {
     FAAR_WAIT_VMCNT(0);
@@ -786,7 +812,7 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
     const int me = again(lane), key = k0 + 32 * kw + (me & 31), at = i0 + 4 * (me >> 5);
     const Seen seen = whole ? Seen{0, 0} : queries_of(key, q_len, off, prefix, window, causal);
     const float* stat = &stats[it & 1][0][32 * (wave >> 1)];
-    masked_dkv_tile<DH, kCap, kBias>(dk, dv, kf, vf, stat, stat + kTok, tile + ra, tile + ca, sc, !whole, at - seen.lo, max(0, seen.hi - seen.lo),
+    masked_dkv_tile<H, kCap, kBias>(dk, dv, kf, vf, stat, stat + kTok, tile + ra, tile + ca, sc, !whole, at - seen.lo, max(0, seen.hi - seen.lo),
                                      static_cast<float>(at + off - key), lane);
   }
   // the two wavefronts of a block of keys: one hands over its dv and finishes dk, the other the reverse
@@ -828,29 +854,29 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
 // A workgroup takes one piece of a sequence's keys for one key / value head and up to 32 of its query heads, which are the columns of
 // the products: blocks of 128 keys, 32 a wavefront, two stages.  The four wavefronts' sums meet through LDS; a sequence of one piece is
 // done, others leave (O, maximum, denominator) of the piece in the workspace for k_masked_join.  Bound by the one pass over the cache.
-template <int DH, int kMode>
+template <class H, int kMode>
 __global__ void __launch_bounds__(256, 1)
 k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
                PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse, float* __restrict__ part) {
-  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][2][Tl::ELEMS];   // [stage][half of the block][k, v]
   __shared__ float ml[3][4][32];
-  if (!plan_is(plan, tag, false)) {
+  const int rep = d.n_q / d.n_kv, per_head = (rep + 31) / 32, cols = d.n_kv * per_head;
+  const int item = blockIdx.x / cols, kvh = blockIdx.x % cols % d.n_kv, h0 = blockIdx.x % cols / d.n_kv * 32;
+  const PlanWords w(plan, z.q_at, item, threadIdx.x & 63);
+  if (!w.is(tag, false)) {
     fill_nan(O, d.Tq, (int64_t)d.n_q * d.dh, d.ldo);
     if (lse) fill_nan(lse, d.Tq * d.n_q);
     return;
   }
-  const int rep = d.n_q / d.n_kv, per_head = (rep + 31) / 32, cols = d.n_kv * per_head;
-  const int item = blockIdx.x / cols, kvh = blockIdx.x % cols % d.n_kv, h0 = blockIdx.x % cols / d.n_kv * 32;
-  if (item >= word(plan + kPlanQItems)) return;
-  const int* w = plan + z.q_at + 8 * item;
-  const int seq = word(w + 0), row0 = word(w + 1), keys = word(w + 2), gap0 = word(w + 3), pieces = word(w + 4);
+  if (item >= w.header(kPlanQItems)) return;
+  const int seq = w.item(0), row0 = w.item(1), keys = w.item(2), gap0 = w.item(3), pieces = w.item(4);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
   const int heads = min(32, rep - h0), head = kvh * rep + h0 + min(n, heads - 1);
   const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped);
 
-  MaskedState<DH> st;
+  MaskedState<H> st;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
     st.qf[ks] = n < heads && ks * 16 + 8 * hi < d.dh ? load_frag16(Q + (int64_t)seq * d.ldq + head * d.dh + ks * 16 + 8 * hi) : bf16x8{};
@@ -872,6 +898,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
     }
   };
   const int blocks = (keys + kPieceKeys - 1) / kPieceKeys;
+  clear_columns<H>(&lds[0][0][0][0], 8, d.dh, tid);
   if (blocks > 0) request(0);
   for (int blk = 0; blk < blocks; ++blk) {
     FAAR_WAIT_VMCNT(0);
@@ -881,7 +908,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
     const int j0 = blk * kPieceKeys + 32 * wave;
     if (j0 >= keys) continue;
     const float gap = static_cast<float>(gap0 - j0 - 4 * hi);
-    masked_block<DH, kMode, 1>(st, k_lds, v_lds, ra, ca, sc, wave & 1, j0 + 32 > keys, j0 + 4 * hi, keys, gap);
+    masked_block<H, kMode, 1>(st, k_lds, v_lds, ra, ca, sc, wave & 1, j0 + 32 > keys, j0 + 4 * hi, keys, gap);
   }
   // the wavefronts' sums on a common maximum
   const float lt = half_sum(st.l), lr = half_sum(st.lr);
@@ -944,8 +971,9 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
 __global__ void __launch_bounds__(128)
 k_masked_join(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, bf16_t* __restrict__ O,
               float* __restrict__ lse) {
-  if (!plan_is(plan, tag, false)) return;              // answered by the kernel before
   const int seq = blockIdx.x / d.n_q, head = blockIdx.x % d.n_q;
+  const PlanWords w(plan, z.q_at, 0, threadIdx.x & 63);
+  if (!w.is(tag, false)) return;                       // answered by the kernel before
   const int first = plan[z.seq_at + 2 * seq], pieces = plan[z.seq_at + 2 * seq + 1];
   if (pieces == 1) return;
   const int64_t step = (int64_t)d.n_q * (d.dh + kPartExtra);
@@ -997,12 +1025,13 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
   const int rep = d.n_q / d.n_kv;
   const int64_t cols = (int64_t)d.n_kv * ((rep + 31) / 32);
   const dim3 grid(static_cast<unsigned>(single ? z.max_q * cols : z.max_q * d.n_q));
-#define FAAR_MF2(DH, M)                                                                                                              \
-  do {                                                                                                                               \
-    if (single) hipLaunchKernelGGL((k_masked_token<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, part);         \
-    else hipLaunchKernelGGL((k_masked_fwd<DH, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, o_low);                 \
+#define FAAR_MF2(H, M)                                                                                                              \
+  do {                                                                                                                              \
+    if (single) hipLaunchKernelGGL((k_masked_token<H, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, part);         \
+    else hipLaunchKernelGGL((k_masked_fwd<H, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, o_low);                 \
   } while (0)
-#define FAAR_MF(M) do { if (d.dh <= 64) FAAR_MF2(64, M); else FAAR_MF2(128, M); } while (0)
+#define FAAR_MF(M) \
+  do { if (d.dh <= 64) FAAR_MF2(Heads64, M); else if (d.dh <= 96) FAAR_MF2(Heads96, M); else FAAR_MF2(Heads128, M); } while (0)
   switch (mode) {
     case kPlain: FAAR_MF(kPlain); break;
     case kBiased: FAAR_MF(kBiased); break;
@@ -1021,12 +1050,13 @@ hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K,
                              const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st) {
   const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv));
-#define FAAR_MB2(DH, C, B)                                                                                                            \
+#define FAAR_MB2(H, C, B)                                                                                                             \
   do {                                                                                                                                \
-    hipLaunchKernelGGL((k_masked_bwd_dq<DH, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ);    \
-    hipLaunchKernelGGL((k_masked_bwd_dkv<DH, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV);         \
+    hipLaunchKernelGGL((k_masked_bwd_dq<H, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ);     \
+    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV);          \
   } while (0)
-#define FAAR_MB(C, B) do { if (d.dh <= 64) FAAR_MB2(64, C, B); else FAAR_MB2(128, C, B); } while (0)
+#define FAAR_MB(C, B) \
+  do { if (d.dh <= 64) FAAR_MB2(Heads64, C, B); else if (d.dh <= 96) FAAR_MB2(Heads96, C, B); else FAAR_MB2(Heads128, C, B); } while (0)
   if (d.cap_a > 0.0f) { if (d.slopes) FAAR_MB(true, true); else FAAR_MB(true, false); }
   else                { if (d.slopes) FAAR_MB(false, true); else FAAR_MB(false, false); }
 #undef FAAR_MB

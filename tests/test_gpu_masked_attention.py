@@ -167,6 +167,8 @@ CASES = {
     "saturated_cap": Case(packed([200, 90]), 2, 2, 64, cap=4.0, gain=8.0),
     "heads_of_8": Case(packed([70, 33]), 4, 2, 8),
     "heads_of_24": Case(packed([70, 130]), 2, 1, 24, cap=8.0),
+    "heads_of_96": Case(packed([70, 130, 64]), 2, 1, 96, cap=8.0),
+    "heads_of_104": Case(packed([200, 33]), 2, 2, 104, causal=False, window=50),
     "heads_of_72": Case(packed([70, 130]), 2, 1, 72, slopes=True),
     "heads_of_120_fused": Case(packed([65, 130]), 3, 3, 120, fused=True),
     "one_key_value_head": Case(packed([129, 40]), 16, 1, 64, cap=30.0),
@@ -246,6 +248,7 @@ TOKENS = {  # lengths of the caches, capacity, n_q, n_kv, dh, window, cap, slope
     "window_of_one": ([5, 300], 320, 2, 1, 128, 1, 0.0, False),
     "many_heads_share": ([40, 333], 384, 80, 2, 64, 0, 0.0, False),
     "long_alone": ([9001], 9100, 2, 1, 128, 0, 30.0, False),
+    "heads_of_96": ([40, 300, 128], 320, 4, 2, 96, 0, 10.0, False),
     "small_caches": ([40, 3, 17], 40, 4, 1, 24, 0, 0.0, False),
     "high_cap": ([300, 200], 300, 2, 2, 128, 0, 100.0, False),
 }
