@@ -1015,7 +1015,7 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
   if (reinterpret_cast<uintptr_t>(a->slopes) & 3u) return FAAR_E_ARG;
   c.z = attention_plan_sizes(a->n_seq, a->Tq, a->Tk, a->n_q, a->n_kv, c.single);
   // the largest grids: work items x heads, and for single tokens one query head of a sequence each
-  if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * a->n_kv > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
+  if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * a->n_q > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
   const int window = a->window > kMaxRows ? 0 : static_cast<int>(a->window);     // wider than any sequence: none
   const int tag[kPlanTagWords] = {0x5A11FAA3, static_cast<int>(a->flags) | (c.single ? 2 : 0), static_cast<int>(a->n_seq), static_cast<int>(a->Tq),
                                   static_cast<int>(a->Tk), window, static_cast<int>(a->n_q), static_cast<int>(a->n_kv)};
@@ -1037,7 +1037,7 @@ int masked_rows(const faar_attention* a) {
 }
 
 size_t masked_ws_bytes(const MaskedCall& c, bool backward) {
-  if (backward) return align256((size_t)c.d.n_q * c.d.Tq * sizeof(float));        // rowsum(dO o) per head and query
+  if (backward) return align256((size_t)masked_bwd_floats(c.z, c.d.n_q, c.d.n_kv, c.d.dh, c.d.Tq, c.d.Tk) * sizeof(float));
   if (c.single) return align256((size_t)c.z.max_q * c.d.n_q * (c.d.dh + kPartExtra) * sizeof(float));
   return 256;                                          // none needed
 }

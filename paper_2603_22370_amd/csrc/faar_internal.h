@@ -209,9 +209,10 @@ constexpr int kPartExtra = 3;
 // o_low: nullable [Tq][n_q * dh], the 8 bits behind each bf16 of O (forward out, not with single tokens; backward in)
 hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
                              const MaskedDims& d, bool single, bf16_t* O, float* lse, uint8_t* o_low, float* part, hipStream_t st);
-// delta: [n_q][Tq]
+// ws: masked_bwd_floats (delta [n_q][Tq], then the parts of dk and dv)
+int64_t masked_bwd_floats(const PlanSizes& z, int64_t n_q, int64_t n_kv, int64_t dh, int64_t Tq, int64_t Tk);
 hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
-                             const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
+                             const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* ws, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st);
 // lse [n_q, T]
 hipError_t launch_attention_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, int64_t n_seq, int64_t S, int64_t n_q,

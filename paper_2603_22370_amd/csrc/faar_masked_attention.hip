@@ -735,18 +735,19 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
   }
 }
 
-// 64 keys of a key / value head a workgroup: wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
+// 64 keys of a key / value head a workgroup (with the head's query heads dealt to `parts` workgroups, whose sums k_masked_join_dkv adds
+// up): wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
 // block of 64 and 2, 3 the others, and the two sums of a block of keys meet through LDS at the end
 template <class H, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                  const float* __restrict__ lse, const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
-                 bf16_t* __restrict__ dK, bf16_t* __restrict__ dV) {
+                 bf16_t* __restrict__ dK, bf16_t* __restrict__ dV, int parts, float* __restrict__ part) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][q, dO]
   __shared__ __attribute__((aligned(16))) float stats[2][2][kTok];         // [stage][lse, delta]
-  const int item = blockIdx.x / d.n_kv, kvh = blockIdx.x % d.n_kv;
+  const int item = blockIdx.x / (d.n_kv * parts), kvh = blockIdx.x % d.n_kv, share = blockIdx.x / d.n_kv % parts;
   const PlanWords w(plan, z.k_at, item, threadIdx.x & 63);
   if (!w.is(tag, true)) {
     fill_nan(dK, d.Tk, (int64_t)d.n_kv * d.dh, d.ldk);
@@ -758,10 +759,9 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
-  const int kw = wave & 1, qw = tid >> 7, rep = d.n_q / d.n_kv;   // qw as a lane's value: it chooses between registers below
+  const int kw = wave & 1, qw = tid >> 7, heads = d.n_q / d.n_kv / parts;   // qw as a lane's value: it chooses between registers below
 
   const int mine = min(32, rows - 32 * kw);            // this wavefront's keys (none: <= 0)
-  const bool live = n < mine;
   const Seen sa = queries_of(k0 + 32 * kw, q_len, off, prefix, window, causal), sb = queries_of(k0 + 32 * kw + mine - 1, q_len, off, prefix, window, causal);
   const int64_t t0 = (int64_t)row0 + 32 * kw + n;
 
@@ -769,7 +769,7 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   f32x16 dk[DT], dv[DT];     // rows = dh, column = key
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
-    const bool on = live && ks * 16 + 8 * hi < d.dh;
+    const bool on = n < mine && ks * 16 + 8 * hi < d.dh;
     const int64_t at = kvh * d.dh + ks * 16 + 8 * hi;
     kf[ks] = on ? load_frag16(K + t0 * d.ldk + at) : bf16x8{};
     vf[ks] = on ? load_frag16(V + t0 * d.ldv + at) : bf16x8{};
@@ -781,19 +781,20 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   }
   // steps: query head of the group (outer) x block of 64 queries first .. end - 1 (inner)
   const int q_lo = queries_of(k0, q_len, off, prefix, window, causal).lo, q_hi = queries_of(k0 + rows - 1, q_len, off, prefix, window, causal).hi;
-  const int first = q_lo / kTok, end = q_hi > q_lo ? (q_hi + kTok - 1) / kTok : first, steps = rep * (end - first);
-  const uint32_t lds0 = lds_addr_of(lds), from_q = Tl::of_lane(d.ldq, tid), from_o = Tl::of_lane(d.ldo, tid);
+  const int first = q_lo / kTok, end = q_hi > q_lo ? (q_hi + kTok - 1) / kTok : first, steps = heads * (end - first);
+  const uint32_t lds0 = lds_addr_of(lds);
   const uint32_t ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
   auto request = [&](int stage, int head, int blk) {
     const uint32_t at = lds0 + stage * (2 * Tl::ELEMS * 2);
-    const int q0 = blk * kTok;
+    const int q0 = blk * kTok, me = again(tid);        // the lane's offsets are formed at every step: no registers to keep them
+    const uint32_t from_q = Tl::of_lane(d.ldq, me), from_o = Tl::of_lane(d.ldo, me);
     copy_tile<DH>(Q, (int64_t)q_start + q0, q_len - q0, d.ldq, (int64_t)head * d.dh, d.dh, from_q, at, wave, tid);
     copy_tile<DH>(dO, (int64_t)q_start + q0, q_len - q0, d.ldo, (int64_t)head * d.dh, d.dh, from_o, at + Tl::ELEMS * 2, wave, tid);
     if (wave < 2)
       dma4((wave == 0 ? lse : delta) + (int64_t)head * d.Tq + q_start + min(q0 + lane, q_len - 1),
            __builtin_amdgcn_readfirstlane(lds_addr_of(stats[stage][wave])));
   };
-  int head = kvh * rep, blk = first;
+  int head = (kvh * parts + share) * heads, blk = first;
   clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
   if (steps > 0) request(0, head, blk);
   for (int it = 0; it < steps; ++it) {
@@ -829,12 +830,24 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   }
   __syncthreads();
   f32x16 sum[DT];
-  const float k = qw == 0 ? d.scale : 1.0f;
+  const float k = qw == 0 && parts == 1 ? d.scale : 1.0f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
     const f32x16 r = take[dt * 64];
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[dt][i] = ((qw == 0 ? dk[dt][i] : dv[dt][i]) + r[i]) * k;
+  }
+  if (parts > 1) {                                     // in float32, [part][dk, dv][row][n_kv * dh]
+    const int me = again(lane);
+    if ((me & 31) >= mine) return;
+    float* out = part + (((int64_t)share * 2 + qw) * d.Tk + row0 + 32 * kw + (me & 31)) * ((int64_t)d.n_kv * d.dh) + kvh * d.dh + 4 * (me >> 5);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (dt * 32 + 8 * i < d.dh)
+          *reinterpret_cast<float4*>(out + dt * 32 + 8 * i) = make_float4(sum[dt][4 * i], sum[dt][4 * i + 1], sum[dt][4 * i + 2], sum[dt][4 * i + 3]);
+    return;
   }
   __syncthreads();                                     // all has been taken: the place is free
   if (mine <= 0) return;
@@ -848,6 +861,33 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
     }
   const int64_t t = (int64_t)row0 + 32 * kw, ld = qw == 0 ? d.ldk : d.ldv;
   RowStage<DH>::flush(stage, lane, mine, d.dh, (qw == 0 ? dK : dV) + t * ld + kvh * d.dh, ld, nullptr, 0);
+}
+
+// dk = scale * sum over parts, dv = sum over parts, in their order, for the rows of one item
+__global__ void __launch_bounds__(256)
+k_masked_join_dkv(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, int parts,
+                  bf16_t* __restrict__ dK, bf16_t* __restrict__ dV) {
+  const PlanWords w(plan, z.k_at, blockIdx.x, threadIdx.x & 63);
+  if (!w.is(tag, true) || (int)blockIdx.x >= w.header(kPlanKItems)) return;      // a wrong plan: answered by the kernel before
+  const int64_t row0 = w.item(0), width = (int64_t)d.n_kv * d.dh;
+  const int rows = w.item(1), c8 = static_cast<int>(width / 8);
+  const bool is_k = blockIdx.y == 0;
+  const float k = is_k ? d.scale : 1.0f;
+  for (int i = blockIdx.z * 256 + threadIdx.x; i < rows * c8; i += 256 * gridDim.z) {
+    const int64_t row = row0 + i / c8, col = i % c8 * 8;
+    float a[8], x[8];
+    const float* p = part + (blockIdx.y * d.Tk + row) * width + col;
+    load8(p, a);
+#pragma unroll 4
+    for (int s = 1; s < parts; ++s) {
+      load8(p + (int64_t)s * 2 * d.Tk * width, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a[j] += x[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) a[j] *= k;
+    W8<bf16_t>::store(is_k ? dK + row * d.ldk + col : dV + row * d.ldv + col, a);
+  }
 }
 
 // ---- one token a sequence ---------------------------------------------------------------------------------------------------------
@@ -1046,14 +1086,32 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
   return hipGetLastError();
 }
 
+// Into how many parts the query heads of a key / value head are dealt: where few key / value heads leave fewer workgroups of 64 keys than
+// fill the device a few times over, equal parts that make them 2048 at most.  dk and dv in us with one part / up to 1024 / 2048 / 4096
+// workgroups: 3 sequences in 8192 tokens, 16 heads of 64 on one 1080 / 311 / 207 / 163 (and 8 to 25 for adding up), of 128 on two 747 / 421
+// / 281 / 292; in 7001, of 64 on four 251 / 146 / 120 / 120; in 2048, of 128 on one 383 / 39 / 40 / 41.
+int masked_bwd_parts(const PlanSizes& z, int64_t n_q, int64_t n_kv) {
+  const int64_t rep = n_q / n_kv, groups = z.max_k * n_kv;
+  int64_t parts = 1;
+  for (int64_t p = 2; p <= rep && groups * p <= 2048; ++p)
+    if (rep % p == 0) parts = p;
+  return static_cast<int>(parts);
+}
+int64_t masked_bwd_floats(const PlanSizes& z, int64_t n_q, int64_t n_kv, int64_t dh, int64_t Tq, int64_t Tk) {
+  const int64_t parts = masked_bwd_parts(z, n_q, n_kv);
+  return round_up(n_q * Tq, 64) + (parts > 1 ? parts * 2 * Tk * n_kv * dh : 0);
+}
+
 hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
-                             const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* delta, bf16_t* dQ, bf16_t* dK,
+                             const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* ws, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st) {
-  const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv));
+  const int parts = masked_bwd_parts(z, d.n_q, d.n_kv);
+  float *delta = ws, *part = ws + round_up(d.n_q * d.Tq, 64);
+  const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv * parts));
 #define FAAR_MB2(H, C, B)                                                                                                             \
   do {                                                                                                                                \
     hipLaunchKernelGGL((k_masked_bwd_dq<H, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ);     \
-    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV);          \
+    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV, parts, part); \
   } while (0)
 #define FAAR_MB(C, B) \
   do { if (d.dh <= 64) FAAR_MB2(Heads64, C, B); else if (d.dh <= 96) FAAR_MB2(Heads96, C, B); else FAAR_MB2(Heads128, C, B); } while (0)
@@ -1061,6 +1119,9 @@ hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K,
   else                { if (d.slopes) FAAR_MB(false, true); else FAAR_MB(false, false); }
 #undef FAAR_MB
 #undef FAAR_MB2
+  if (hipError_t e = hipGetLastError()) return e;
+  if (parts > 1)
+    hipLaunchKernelGGL(k_masked_join_dkv, dim3(static_cast<unsigned>(z.max_k), 2, 4), dim3(256), 0, st, plan, tag, z, d, part, parts, dK, dV);
   return hipGetLastError();
 }
 

@@ -172,6 +172,14 @@ CASES = {
     "heads_of_72": Case(packed([70, 130]), 2, 1, 72, slopes=True),
     "heads_of_120_fused": Case(packed([65, 130]), 3, 3, 120, fused=True),
     "one_key_value_head": Case(packed([129, 40]), 16, 1, 64, cap=30.0),
+    # more work items than the device holds at once
+    "many": Case(packed([130, 1, 200, 128, 65, 250] * 3, gap=1), 32, 8, 64, cap=5.0),
+    "many_128": Case(packed([130, 1, 200, 128, 65, 250] * 2), 32, 4, 128, slopes=True),
+    "many_whole_96": Case(packed([130, 33, 200, 129] * 3), 32, 32, 88, causal=False),
+    "many_windows": Case(packed([300] * 5, prefix=40), 32, 2, 72, window=70, cap=90.0, slopes=True, fused=True),
+    # a workgroup of dk and dv takes both query heads of a key / value head; two of its four; (above: one)
+    "pairs_of_heads": Case(packed([130, 64, 200, 129, 65] * 3), 64, 32, 32, cap=5.0),
+    "quads_of_heads": Case(packed([130, 64, 200, 129, 65] * 3), 64, 16, 24, window=100),
     "long": Case(packed([1500, 37]), 1, 1, 64, cap=30.0),
 }
 
