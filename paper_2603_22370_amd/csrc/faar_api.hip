@@ -1008,6 +1008,7 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
   if (a->n_seq <= 0 || a->n_seq > ((int64_t)1 << 20) || a->Tq <= 0 || a->Tk <= 0 || a->Tq > kMaxRows || a->Tk > kMaxRows) return FAAR_E_SHAPE;
   if ((c.single && a->Tq != a->n_seq) || (!a->k_start && a->Tk != a->Tq)) return FAAR_E_SHAPE;
   if (a->n_q <= 0 || a->n_kv <= 0 || a->n_q % a->n_kv != 0 || a->n_q > 4096 || a->dh <= 0 || a->dh % 8 != 0 || a->dh > 128) return FAAR_E_SHAPE;
+  if (a->n_q / a->n_kv * ((a->Tq + 63) / 64) > kMaxRows) return FAAR_E_SHAPE;     // what one tile of keys walks
   if (a->window < 0 || (a->flags & ~(uint32_t)FAAR_ATTENTION_CAUSAL)) return FAAR_E_ARG;
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale) || !(a->cap >= 0.0f) || !std::isfinite(a->cap)) return FAAR_E_ARG;
   for (const int32_t* p : {a->q_start, a->q_len, a->k_start, a->k_len, a->prefix})
@@ -1015,7 +1016,7 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
   if (reinterpret_cast<uintptr_t>(a->slopes) & 3u) return FAAR_E_ARG;
   c.z = attention_plan_sizes(a->n_seq, a->Tq, a->Tk, a->n_q, a->n_kv, c.single);
   // the largest grids: work items x heads, and for single tokens one query head of a sequence each
-  if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * a->n_q > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
+  if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * 2 * a->n_kv > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
   const int window = a->window > kMaxRows ? 0 : static_cast<int>(a->window);     // wider than any sequence: none
   const int tag[kPlanTagWords] = {0x5A11FAA3, static_cast<int>(a->flags) | (c.single ? 2 : 0), static_cast<int>(a->n_seq), static_cast<int>(a->Tq),
                                   static_cast<int>(a->Tk), window, static_cast<int>(a->n_q), static_cast<int>(a->n_kv)};
@@ -1037,9 +1038,8 @@ int masked_rows(const faar_attention* a) {
 }
 
 size_t masked_ws_bytes(const MaskedCall& c, bool backward) {
-  if (backward) return align256((size_t)masked_bwd_floats(c.z, c.d.n_q, c.d.n_kv, c.d.dh, c.d.Tq, c.d.Tk) * sizeof(float));
-  if (c.single) return align256((size_t)c.z.max_q * c.d.n_q * (c.d.dh + kPartExtra) * sizeof(float));
-  return 256;                                          // none needed
+  const int64_t n = backward ? masked_bwd_floats(c.z, c.d) : masked_fwd_floats(c.z, c.d, c.single);
+  return align256(std::max<size_t>(1, (size_t)n * sizeof(float)));      // never 0, which says that the description is invalid
 }
 
 }  // namespace

@@ -189,12 +189,13 @@ constexpr int kRopeMaxHalf = 128;       // frequencies of a head
 struct RopeAxes { double turns[kRopeMaxHalf]; uint8_t axis[kRopeMaxHalf]; };   // turns per position and position axis of each frequency
 hipError_t launch_rope_axes(const RopeTensor& q, const RopeTensor& k, int64_t T, int dh, int half, const int32_t* pos, const RopeAxes& ax,
                             bool inverse, bool pairs, bool copy_rest, hipStream_t st);
-// Attention under masks.  The plan is an array of ints: a tag (what it was made for), its counts, then the work items, 8 words each.
+// Attention under masks.  The plan is an array of ints: a tag (what it was made for), its counts, then the work items, kItemWords words each, and lists of tiles in pieces.
 enum { kTagMagic = 0, kTagFlags, kTagSeqs, kTagTq, kTagTk, kTagWindow, kTagNq, kTagNkv, kPlanTagWords };   // flags: 1 causal, 2 single tokens
-enum { kPlanBad = kPlanTagWords, kPlanNoBackward, kPlanQItems, kPlanKItems };
+enum { kPlanBad = kPlanTagWords, kPlanNoBackward, kPlanQItems, kPlanKItems, kPlanQJoins, kPlanKJoins };
+constexpr int kItemWords = 16;
 constexpr int kPieceKeys = 128;         // single tokens: keys of a block
 struct PlanTag { int w[kPlanTagWords]; };
-struct PlanSizes { int q_at, k_at, seq_at, target; int64_t max_q, max_k, words; };   // places (words), bounds of the item counts
+struct PlanSizes { int q_at, k_at, seq_at, join_at[2], target, extra_q, extra_k; int64_t max_q, max_k, words; };   // places (words), bounds of counts
 struct MaskedDims {
   int n_q, n_kv, dh;
   int64_t Tq, Tk, ldq, ldk, ldv, ldo;   // rows; elements between rows
@@ -204,13 +205,14 @@ struct MaskedDims {
 PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, bool single);
 hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int* k_start, const int* k_len, const int* prefix, const PlanTag& tag,
                                  const PlanSizes& z, int* plan, hipStream_t st);
-// part (single tokens): [max_q][n_q][dh + kPartExtra]: a piece's sum, maximum and two denominators
+// part: masked_fwd_floats; a piece's sums are followed by a maximum and two denominators
 constexpr int kPartExtra = 3;
 // o_low: nullable [Tq][n_q * dh], the 8 bits behind each bf16 of O (forward out, not with single tokens; backward in)
 hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
                              const MaskedDims& d, bool single, bf16_t* O, float* lse, uint8_t* o_low, float* part, hipStream_t st);
-// ws: masked_bwd_floats (delta [n_q][Tq], then the parts of dk and dv)
-int64_t masked_bwd_floats(const PlanSizes& z, int64_t n_q, int64_t n_kv, int64_t dh, int64_t Tq, int64_t Tk);
+// ws: masked_bwd_floats (delta [n_q][Tq], then sums of pieces)
+int64_t masked_fwd_floats(const PlanSizes& z, const MaskedDims& d, bool single);
+int64_t masked_bwd_floats(const PlanSizes& z, const MaskedDims& d);
 hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
                              const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* ws, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st);

@@ -108,7 +108,8 @@ __device__ __forceinline__ Seen queries_of(int j, int q_len, int off, int prefix
 }
 
 // ---- the plan -----------------------------------------------------------------------------------------------------------------
-constexpr int kPlanThreads = 1024, kBuckets = 128;
+constexpr int kJoinThreads = 1024;     // a workgroup that adds up pieces
+constexpr int kPlanThreads = 1024, kBuckets = 128, kLeastPiece = 8;
 
 __device__ __forceinline__ bool inside(int start, int len, int T) { return start >= 0 && len >= 0 && start <= T && len <= T - start; }
 
@@ -119,10 +120,12 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
   const bool causal = tag.w[kTagFlags] & 1, single = tag.w[kTagFlags] & 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __shared__ unsigned long long sums[2];              // rows of q, of k
-  __shared__ int most[2], bad, hist[2][kBuckets], scan[kPlanThreads], carry;
+  __shared__ unsigned long long total[2];
+  __shared__ float per_cost[2];
+  __shared__ int longest[2], most_of_piece[2], slots[2], joins[2], bad, hist[2][kBuckets], scan[kPlanThreads], carry;
   if (tid < 2) {
-    sums[tid] = 0;
-    most[tid] = 0;
+    sums[tid] = total[tid] = 0;
+    longest[tid] = slots[tid] = joins[tid] = 0;
     bad = 0;
     carry = 0;
   }
@@ -142,8 +145,6 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
     }
     atomicAdd(&sums[0], static_cast<unsigned long long>(single ? blocks_of(b) : ql));
     atomicAdd(&sums[1], static_cast<unsigned long long>(kl));
-    atomicMax(&most[0], (kl + kTok - 1) / kTok);
-    atomicMax(&most[1], (ql + kTok - 1) / kTok);
   }
   __syncthreads();
   // overlapping sequences would need more items than there is room for
@@ -177,13 +178,12 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
         plan[z.seq_at + 2 * b + 1] = n;
         for (int i = 0; i < n; ++i) {
           const int j0 = min(kl, lo + i * per * kPieceKeys), j1 = min(kl, j0 + per * kPieceKeys);
-          int* w = plan + z.q_at + 8 * (first + i);
+          int* w = plan + z.q_at + kItemWords * (first + i);
           w[0] = b;
           w[1] = k_start[b] + j0;
           w[2] = j1 - j0;
           w[3] = kl - 1 - j0;                          // distance of the piece's first key
           w[4] = n;
-          w[5] = w[6] = w[7] = 0;
         }
       }
       __syncthreads();
@@ -197,45 +197,84 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
     return;
   }
 
-  // two passes over all items, a wavefront a sequence and a lane a tile: count the items of each cost, then place them, the most
-  // expensive first.  Items of one cost come in no particular order; no result depends on it.
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int b = wave; b < n_seq; b += kPlanThreads / 64) {
+  // Passes over all tiles, a wavefront a sequence and a lane a tile: what they cost in all; the items of each cost, counted; the items,
+  // placed, the most expensive first.  A tile that costs more than a slot's share of the device is cut into pieces of equal length along
+  // what its workgroup walks (keys; query heads and queries), which leave float32 sums for the join kernels.  A piece is 8 blocks of 64
+  // at least, and there are at most z.extra_* more pieces than tiles.  Items of one cost, and the places of sums, come in no particular
+  // order; no result depends on it.
+  const int rep = tag.w[kTagNq] / tag.w[kTagNkv];
+  // a wavefront a sequence; of few sequences, all wavefronts share the tiles of each
+  const int stride = n_seq < kPlanThreads / 64 ? kPlanThreads : 64, lead = stride == 64 ? lane : tid;
+  for (int pass = -1; pass < 2; ++pass) {
+    unsigned long long sum[2] = {0, 0};
+    int longest_seen[2] = {0, 0};
+    for (int b = stride == 64 ? wave : 0; b < n_seq; b += stride == 64 ? kPlanThreads / 64 : 1) {
       const int ql = q_len[b], kl = k_len[b], qs = q_start[b], ks = k_start[b], off = kl - ql;
       const int pre = prefix ? min(prefix[b], kl) : 0;
-      for (int t = lane; t < (ql + 127) / 128; t += 64) {
+      auto tile = [&](int kind, int row0, int rows, int from, int to, auto&& fill) {
+        const int len = to - from;
+        if (pass < 0) {
+          sum[kind] += len;
+          longest_seen[kind] = max(longest_seen[kind], len);
+          return;
+        }
+        const int pieces = len <= most_of_piece[kind] ? 1 : (len + most_of_piece[kind] - 1) / most_of_piece[kind];
+        const int each = pieces == 1 ? len : len / pieces, more = pieces == 1 ? 0 : len - each * pieces;      // the first `more` are one longer
+        int slot = -1;
+        if (pass == 1 && pieces > 1) {
+          slot = atomicAdd(&slots[kind], pieces);
+          int* w = plan + z.join_at[kind] + 8 * atomicAdd(&joins[kind], 1);
+          w[0] = row0; w[1] = rows; w[2] = slot; w[3] = pieces;
+        }
+        for (int i = 0; i < pieces; ++i) {
+          const int p0 = from + i * each + min(i, more), p1 = p0 + each + (i < more ? 1 : 0);
+          // 0: the most expensive; the product is below kBuckets for every cost up to the longest, whatever its rounding
+          const int bucket = kBuckets - 1 - min(kBuckets - 1, static_cast<int>(static_cast<float>(p1 - p0) * per_cost[kind]));
+          const int at = atomicAdd(&hist[kind][bucket], 1);
+          if (pass == 1) fill(plan + (kind ? z.k_at : z.q_at) + kItemWords * at, p0, p1, slot < 0 ? -1 : slot + i);
+        }
+      };
+      for (int t = lead; t < (ql + 127) / 128; t += stride) {
         const int r0 = 128 * t, n = min(128, ql - r0), p = off + r0;
         const int lo = keys_of(p, kl, pre, window, causal).lo, hi = keys_of(p + n - 1, kl, pre, window, causal).hi;
-        const int b0 = hi > lo ? lo / kTok : 0, b1 = hi > lo ? (hi + kTok - 1) / kTok : 0;
-        const int bucket = kBuckets - 1 - static_cast<int>(static_cast<int64_t>(b1 - b0) * kBuckets / (most[0] + 1));
-        const int at = atomicAdd(&hist[0][bucket], 1);
-        if (pass == 1) {
-          int* w = plan + z.q_at + 8 * at;
-          w[0] = qs + r0; w[1] = n; w[2] = p; w[3] = ks; w[4] = kl; w[5] = pre; w[6] = b0; w[7] = b1;
-        }
+        tile(0, qs + r0, n, hi > lo ? lo / kTok : 0, hi > lo ? (hi + kTok - 1) / kTok : 0, [&](int* w, int b0, int b1, int slot) {
+          w[0] = qs + r0; w[1] = n; w[2] = p; w[3] = ks; w[4] = kl; w[5] = pre; w[6] = b0; w[7] = b1; w[8] = slot;
+        });
       }
       if (!keys_once) continue;
-      for (int t = lane; t < (kl + kTok - 1) / kTok; t += 64) {
+      for (int t = lead; t < (kl + kTok - 1) / kTok; t += stride) {
         const int k0 = kTok * t, n = min(kTok, kl - k0);
         const int lo = queries_of(k0, ql, off, pre, window, causal).lo, hi = queries_of(k0 + n - 1, ql, off, pre, window, causal).hi;
-        const int cost = hi > lo ? (hi + kTok - 1) / kTok - lo / kTok : 0;
-        const int bucket = kBuckets - 1 - static_cast<int>(static_cast<int64_t>(cost) * kBuckets / (most[1] + 1));
-        const int at = atomicAdd(&hist[1][bucket], 1);
-        if (pass == 1) {
-          int* w = plan + z.k_at + 8 * at;
-          w[0] = ks + k0; w[1] = n; w[2] = k0; w[3] = qs; w[4] = ql; w[5] = off; w[6] = pre; w[7] = 0;
-        }
+        const int blocks = hi > lo ? (hi + kTok - 1) / kTok - lo / kTok : 0;
+        tile(1, ks + k0, n, 0, rep * blocks, [&](int* w, int s0, int s1, int slot) {
+          w[0] = ks + k0; w[1] = n; w[2] = k0; w[3] = qs; w[4] = ql; w[5] = off; w[6] = pre; w[7] = s0; w[8] = s1; w[9] = slot;
+        });
       }
     }
+    if (pass < 0)
+      for (int kind = 0; kind < 2; ++kind)
+        if (sum[kind]) {
+          atomicAdd(&total[kind], sum[kind]);
+          atomicMax(&longest[kind], longest_seen[kind]);
+        }
     __syncthreads();
-    if (pass == 0 && tid < 2) {                        // counts -> first place of each cost
-      int at = 0;
-      for (int i = 0; i < kBuckets; ++i) {
-        const int n = hist[tid][i];
-        hist[tid][i] = at;
-        at += n;
+    if (tid < 2) {
+      const int extra = tid == 0 ? z.extra_q : z.extra_k;
+      if (pass < 0) {
+        const unsigned long long share = extra > 0 ? (total[tid] + extra - 1) / extra : 0x7FFFFFFFull;
+        most_of_piece[tid] = static_cast<int>(min(max(share, static_cast<unsigned long long>(kLeastPiece)), 0x3FFFFFFFull));
+        per_cost[tid] = static_cast<float>(kBuckets) / static_cast<float>(min(longest[tid], most_of_piece[tid]) + 1);
+      } else if (pass == 0) {                          // counts -> first place of each cost
+        int at = 0;
+        for (int i = 0; i < kBuckets; ++i) {
+          const int n = hist[tid][i];
+          hist[tid][i] = at;
+          at += n;
+        }
+        plan[tid == 0 ? kPlanQItems : kPlanKItems] = at;
+      } else {
+        plan[tid == 0 ? kPlanQJoins : kPlanKJoins] = joins[tid];
       }
-      plan[tid == 0 ? kPlanQItems : kPlanKItems] = at;
     }
     __syncthreads();
   }
@@ -247,12 +286,13 @@ __device__ __forceinline__ int again(int x) {
   return x;
 }
 
-// A workgroup's look at the plan: one load brings the header (lanes 0 .. 15) and the words of its item (16 .. 23), which lie inside the
+// A workgroup's look at the plan: one load brings the header (lanes 0 .. 15) and the words of its item (16 .. 31), which lie inside the
 // plan's memory whether or not that many items are in use
-struct PlanWords {
+template <int WORDS>
+struct PlanLook {
   int w;
-  __device__ __forceinline__ PlanWords(const int* __restrict__ plan, int items_at, int item, int lane)
-      : w(plan[lane < 16 ? lane : items_at + 8 * item + (lane & 7)]) {}
+  __device__ __forceinline__ PlanLook(const int* __restrict__ plan, int items_at, int item, int lane)
+      : w(plan[lane < 16 ? lane : items_at + WORDS * item + (lane & (WORDS - 1))]) {}
   __device__ __forceinline__ int header(int i) const { return __builtin_amdgcn_readlane(w, i); }
   __device__ __forceinline__ int item(int i) const { return __builtin_amdgcn_readlane(w, 16 + i); }
   // Is this the plan of the call's description?  What is not is answered with NaN.
@@ -263,6 +303,7 @@ struct PlanWords {
     return ok;
   }
 };
+typedef PlanLook<kItemWords> PlanWords;
 __device__ __forceinline__ void fill_nan(bf16_t* p, int64_t rows, int64_t width, int64_t ld) {
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
     for (int64_t c = threadIdx.x; c < width; c += blockDim.x) p[r * ld + c] = 0x7FC0;
@@ -434,6 +475,19 @@ struct RowStage {
   }
 };
 
+// a wavefront's 32 rows x dh as float32 sums of a piece, rows dh apart
+template <class H>
+__device__ __forceinline__ void leave_sums(const f32x16 (&acc)[H::DT], float* out, int rows, int dh, int lane) {
+  const int n = lane & 31, hi = lane >> 5;
+  if (n >= rows) return;
+#pragma unroll
+  for (int dt = 0; dt < H::DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (dt * 32 + 8 * j < dh)
+        *reinterpret_cast<float4*>(out + n * dh + dt * 32 + 8 * j + 4 * hi) = make_float4(acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]);
+}
+
 // the float of a bf16 and its byte
 __device__ __forceinline__ float with_low(uint32_t bf16_top, uint32_t byte) {
   return __uint_as_float(bf16_top + (static_cast<uint32_t>(static_cast<int>(byte << 24) >> 24) << 8));
@@ -442,7 +496,7 @@ __device__ __forceinline__ float with_low(uint32_t bf16_top, uint32_t byte) {
 template <class H, int kMode>
 __global__ void __launch_bounds__(256, 2)
 k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
-             PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse, uint8_t* __restrict__ o_low) {
+             PlanSizes z, MaskedDims d, bf16_t* __restrict__ O, float* __restrict__ lse, uint8_t* __restrict__ o_low, float* __restrict__ part) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
@@ -454,7 +508,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
     return;
   }
   if (item >= w.header(kPlanQItems)) return;
-  const int row0 = w.item(0), rows = w.item(1), pos0 = w.item(2), k_start = w.item(3), k_len = w.item(4), prefix = w.item(5), kb0 = w.item(6), kb1 = w.item(7);
+  const int row0 = w.item(0), rows = w.item(1), pos0 = w.item(2), k_start = w.item(3), k_len = w.item(4), prefix = w.item(5), kb0 = w.item(6), kb1 = w.item(7), slot = w.item(8);
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
@@ -499,6 +553,17 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
   __syncthreads();                                     // the tiles have been read: their place is free
   if (mine <= 0) return;
   const float lt = half_sum(st.l), lr = half_sum(st.lr);
+  if (slot >= 0) {                                     // a piece: [128 rows][dh] sums, then maximum and denominators of the rows
+    float* at = part + ((int64_t)slot * d.n_q + head) * (128 * (d.dh + kPartExtra));
+    leave_sums<H>(st.oacc, at + 32 * wave * d.dh, mine, d.dh, lane);
+    float* m = at + 128 * d.dh + 32 * wave + n;
+    if (hi == 0 && n < mine) {
+      m[0] = st.mc;
+      m[128] = lt;
+      m[256] = lr;
+    }
+    return;
+  }
   const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;      // a query that sees no key: 0
   char* stage = reinterpret_cast<char*>(lds) + wave * RowStage<DH>::BYTES;
   static_assert(4 * RowStage<DH>::BYTES <= sizeof(lds), "rows fit in the stages");
@@ -514,6 +579,39 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
   const int64_t t = (int64_t)row0 + 32 * wave, width = (int64_t)d.n_q * d.dh;
   if (lse && hi == 0 && n < mine) lse[(int64_t)head * d.Tq + t + n] = lt > 0.0f ? st.mc * kLn2 + logf(lt) : -INFINITY;
   RowStage<DH>::flush(stage, lane, mine, d.dh, O + t * d.ldo + head * d.dh, d.ldo, o_low ? o_low + t * width + head * d.dh : nullptr, width);
+}
+
+// the pieces of a tile's queries, in their order; one query head a workgroup
+__global__ void __launch_bounds__(kJoinThreads)
+k_masked_join_fwd(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, bf16_t* __restrict__ O,
+                  float* __restrict__ lse, uint8_t* __restrict__ o_low) {
+  const int item = blockIdx.x / d.n_q, head = blockIdx.x % d.n_q;
+  const PlanLook<8> w(plan, z.join_at[0], item, threadIdx.x & 63);
+  if (!w.is(tag, false) || item >= w.header(kPlanQJoins)) return;      // a wrong plan: answered by the kernel before
+  const int64_t row0 = w.item(0), step = (int64_t)d.n_q * 128 * (d.dh + kPartExtra), width = (int64_t)d.n_q * d.dh;
+  const int rows = w.item(1), pieces = w.item(3), c4 = d.dh / 4;
+  const float* first = part + ((int64_t)w.item(2) * d.n_q + head) * (128 * (d.dh + kPartExtra));
+  for (int i = threadIdx.x; i < rows * c4; i += kJoinThreads) {
+    const int row = i / c4, col = i % c4 * 4;
+    const float *sums = first + row * d.dh + col, *stats = first + 128 * d.dh + row;
+    float m = kLowest, l = 0.0f, r = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = 0; p < pieces; ++p) m = fmaxf(m, stats[p * step]);
+#pragma unroll 2
+    for (int p = 0; p < pieces; ++p) {
+      const float f = fast_exp2(stats[p * step] - m);
+      const float4 v = *reinterpret_cast<const float4*>(sums + p * step);
+      l += stats[p * step + 128] * f;
+      r += stats[p * step + 256] * f;
+      x[0] += v.x * f; x[1] += v.y * f; x[2] += v.z * f; x[3] += v.w * f;
+    }
+    const float inv = r > 0.0f ? 1.0f / r : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= inv;
+    const uint2 o = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    *reinterpret_cast<uint2*>(O + (row0 + row) * d.ldo + head * d.dh + col) = o;
+    if (o_low) *reinterpret_cast<uint32_t*>(o_low + (row0 + row) * width + head * d.dh + col) = low_bytes(x, o);
+    if (lse && col == 0) lse[(int64_t)head * d.Tq + row0 + row] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+  }
 }
 
 // ---- backward: dq ---------------------------------------------------------------------------------------------------------------
@@ -581,8 +679,8 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
 template <class H, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
-                const bf16_t* __restrict__ O, const uint8_t* __restrict__ o_low, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
-                float* __restrict__ delta, bf16_t* __restrict__ dQ) {
+                const bf16_t* __restrict__ O, const uint8_t* __restrict__ o_low, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag,
+                PlanSizes z, MaskedDims d, float* __restrict__ delta, bf16_t* __restrict__ dQ, float* __restrict__ part) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][k, v]
@@ -593,7 +691,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
     return;
   }
   if (item >= w.header(kPlanQItems)) return;
-  const int row0 = w.item(0), rows = w.item(1), pos0 = w.item(2), k_start = w.item(3), k_len = w.item(4), prefix = w.item(5), kb0 = w.item(6), kb1 = w.item(7);
+  const int row0 = w.item(0), rows = w.item(1), pos0 = w.item(2), k_start = w.item(3), k_len = w.item(4), prefix = w.item(5), kb0 = w.item(6), kb1 = w.item(7), slot = w.item(8);
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
@@ -660,6 +758,10 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
   }
   __syncthreads();
   if (mine <= 0) return;
+  if (slot >= 0) {                                     // a piece: [128 rows][dh] sums
+    leave_sums<H>(acc, part + (((int64_t)slot * d.n_q + head) * 128 + 32 * wave) * d.dh, mine, d.dh, lane);
+    return;
+  }
   char* stage = reinterpret_cast<char*>(lds) + wave * RowStage<DH>::BYTES;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -735,19 +837,18 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
   }
 }
 
-// 64 keys of a key / value head a workgroup (with the head's query heads dealt to `parts` workgroups, whose sums k_masked_join_dkv adds
-// up): wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
+// 64 keys of a key / value head a workgroup: wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
 // block of 64 and 2, 3 the others, and the two sums of a block of keys meet through LDS at the end
 template <class H, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                  const float* __restrict__ lse, const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
-                 bf16_t* __restrict__ dK, bf16_t* __restrict__ dV, int parts, float* __restrict__ part) {
+                 bf16_t* __restrict__ dK, bf16_t* __restrict__ dV, float* __restrict__ part) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][q, dO]
   __shared__ __attribute__((aligned(16))) float stats[2][2][kTok];         // [stage][lse, delta]
-  const int item = blockIdx.x / (d.n_kv * parts), kvh = blockIdx.x % d.n_kv, share = blockIdx.x / d.n_kv % parts;
+  const int item = blockIdx.x / d.n_kv, kvh = blockIdx.x % d.n_kv;
   const PlanWords w(plan, z.k_at, item, threadIdx.x & 63);
   if (!w.is(tag, true)) {
     fill_nan(dK, d.Tk, (int64_t)d.n_kv * d.dh, d.ldk);
@@ -755,11 +856,11 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
     return;
   }
   if (item >= w.header(kPlanKItems)) return;
-  const int row0 = w.item(0), rows = w.item(1), k0 = w.item(2), q_start = w.item(3), q_len = w.item(4), off = w.item(5), prefix = w.item(6);
+  const int row0 = w.item(0), rows = w.item(1), k0 = w.item(2), q_start = w.item(3), q_len = w.item(4), off = w.item(5), prefix = w.item(6), step0 = w.item(7), steps = w.item(8) - step0, slot = w.item(9);
   const int window = tag.w[kTagWindow];
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
-  const int kw = wave & 1, qw = tid >> 7, heads = d.n_q / d.n_kv / parts;   // qw as a lane's value: it chooses between registers below
+  const int kw = wave & 1, qw = tid >> 7, heads = d.n_q / d.n_kv;   // qw as a lane's value: it chooses between registers below
 
   const int mine = min(32, rows - 32 * kw);            // this wavefront's keys (none: <= 0)
   const Seen sa = queries_of(k0 + 32 * kw, q_len, off, prefix, window, causal), sb = queries_of(k0 + 32 * kw + mine - 1, q_len, off, prefix, window, causal);
@@ -779,9 +880,9 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
     dk[dt] = zero16();
     dv[dt] = zero16();
   }
-  // steps: query head of the group (outer) x block of 64 queries first .. end - 1 (inner)
+  // steps: query head of the group (outer) x block of 64 queries first .. end - 1 (inner), of which the item takes a run
   const int q_lo = queries_of(k0, q_len, off, prefix, window, causal).lo, q_hi = queries_of(k0 + rows - 1, q_len, off, prefix, window, causal).hi;
-  const int first = q_lo / kTok, end = q_hi > q_lo ? (q_hi + kTok - 1) / kTok : first, steps = heads * (end - first);
+  const int first = q_lo / kTok, end = q_hi > q_lo ? (q_hi + kTok - 1) / kTok : first;
   const uint32_t lds0 = lds_addr_of(lds);
   const uint32_t ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
   auto request = [&](int stage, int head, int blk) {
@@ -794,7 +895,11 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
       dma4((wave == 0 ? lse : delta) + (int64_t)head * d.Tq + q_start + min(q0 + lane, q_len - 1),
            __builtin_amdgcn_readfirstlane(lds_addr_of(stats[stage][wave])));
   };
-  int head = (kvh * parts + share) * heads, blk = first;
+  int head = kvh * heads, blk = first;
+  if (steps > 0) {
+    head += step0 / (end - first);
+    blk += step0 % (end - first);
+  }
   clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
   if (steps > 0) request(0, head, blk);
   for (int it = 0; it < steps; ++it) {
@@ -830,23 +935,15 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   }
   __syncthreads();
   f32x16 sum[DT];
-  const float k = qw == 0 && parts == 1 ? d.scale : 1.0f;
+  const float k = qw == 0 && slot < 0 ? d.scale : 1.0f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
     const f32x16 r = take[dt * 64];
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[dt][i] = ((qw == 0 ? dk[dt][i] : dv[dt][i]) + r[i]) * k;
   }
-  if (parts > 1) {                                     // in float32, [part][dk, dv][row][n_kv * dh]
-    const int me = again(lane);
-    if ((me & 31) >= mine) return;
-    float* out = part + (((int64_t)share * 2 + qw) * d.Tk + row0 + 32 * kw + (me & 31)) * ((int64_t)d.n_kv * d.dh) + kvh * d.dh + 4 * (me >> 5);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (dt * 32 + 8 * i < d.dh)
-          *reinterpret_cast<float4*>(out + dt * 32 + 8 * i) = make_float4(sum[dt][4 * i], sum[dt][4 * i + 1], sum[dt][4 * i + 2], sum[dt][4 * i + 3]);
+  if (slot >= 0) {                                     // a piece: [dk, dv][64 rows][dh] sums
+    leave_sums<H>(sum, part + ((((int64_t)slot * d.n_kv + kvh) * 2 + qw) * 64 + 32 * kw) * d.dh, mine, d.dh, again(lane));
     return;
   }
   __syncthreads();                                     // all has been taken: the place is free
@@ -863,30 +960,35 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   RowStage<DH>::flush(stage, lane, mine, d.dh, (qw == 0 ? dK : dV) + t * ld + kvh * d.dh, ld, nullptr, 0);
 }
 
-// dk = scale * sum over parts, dv = sum over parts, in their order, for the rows of one item
-__global__ void __launch_bounds__(256)
-k_masked_join_dkv(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, int parts,
-                  bf16_t* __restrict__ dK, bf16_t* __restrict__ dV) {
-  const PlanWords w(plan, z.k_at, blockIdx.x, threadIdx.x & 63);
-  if (!w.is(tag, true) || (int)blockIdx.x >= w.header(kPlanKItems)) return;      // a wrong plan: answered by the kernel before
-  const int64_t row0 = w.item(0), width = (int64_t)d.n_kv * d.dh;
-  const int rows = w.item(1), c8 = static_cast<int>(width / 8);
-  const bool is_k = blockIdx.y == 0;
-  const float k = is_k ? d.scale : 1.0f;
-  for (int i = blockIdx.z * 256 + threadIdx.x; i < rows * c8; i += 256 * gridDim.z) {
-    const int64_t row = row0 + i / c8, col = i % c8 * 8;
+// The pieces of a tile's rows, in their order: out = k * sum, of dq (kind 0, 128 rows a slot) or of dk and dv (kind 1, 64 rows of either);
+// one head a workgroup
+template <int kind>
+__global__ void __launch_bounds__(kJoinThreads)
+k_masked_join_grad(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, bf16_t* __restrict__ A,
+                   bf16_t* __restrict__ B) {
+  constexpr int kSets = kind ? 2 : 1, kHeight = kind ? 64 : 128;
+  const int heads = kind ? d.n_kv : d.n_q, item = blockIdx.x / heads, head = blockIdx.x % heads;
+  const PlanLook<8> w(plan, z.join_at[kind], item, threadIdx.x & 63);
+  if (!w.is(tag, true) || item >= w.header(kind ? kPlanKJoins : kPlanQJoins)) return;      // a wrong plan: answered by the kernel before
+  const int64_t row0 = w.item(0), step = (int64_t)heads * kSets * kHeight * d.dh;
+  const int rows = w.item(1), pieces = w.item(3), c8 = d.dh / 8;
+  const float* first = part + ((int64_t)w.item(2) * heads + head) * kSets * kHeight * d.dh;
+  for (int i = threadIdx.x; i < kSets * rows * c8; i += kJoinThreads) {
+    const int set = i / (rows * c8), row = i / c8 % rows, col = i % c8 * 8;
+    const float* p = first + (set * kHeight + row) * d.dh + col;
     float a[8], x[8];
-    const float* p = part + (blockIdx.y * d.Tk + row) * width + col;
     load8(p, a);
-#pragma unroll 4
-    for (int s = 1; s < parts; ++s) {
-      load8(p + (int64_t)s * 2 * d.Tk * width, x);
+#pragma unroll 2
+    for (int j = 1; j < pieces; ++j) {
+      load8(p + j * step, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) a[j] += x[j];
+      for (int e = 0; e < 8; ++e) a[e] += x[e];
     }
+    if (set == 0)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] *= k;
-    W8<bf16_t>::store(is_k ? dK + row * d.ldk + col : dV + row * d.ldv + col, a);
+      for (int e = 0; e < 8; ++e) a[e] *= d.scale;
+    const int64_t ld = kind == 0 ? d.ldq : set == 0 ? d.ldk : d.ldv;
+    W8<bf16_t>::store((set == 0 ? A : B) + (row0 + row) * ld + head * d.dh + col, a);
   }
 }
 
@@ -1040,15 +1142,46 @@ PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_
     const int64_t cols = n_kv * ((n_q / n_kv + 31) / 32);
     z.target = static_cast<int>((512 + cols - 1) / cols);
     z.max_q = n_seq + z.target;
-    z.seq_at = static_cast<int>(z.q_at + 8 * z.max_q);
+    z.seq_at = static_cast<int>(z.q_at + kItemWords * z.max_q);
     z.words = z.seq_at + 2 * n_seq;
     return z;
   }
-  z.max_q = Tq / 128 + n_seq;
-  z.max_k = Tk / kTok + n_seq;
-  z.k_at = static_cast<int>(z.q_at + 8 * z.max_q);
-  z.words = z.k_at + 8 * z.max_k;
+  // Tiles in pieces: where the rows make fewer workgroups than the device holds a time and a half (768 of 128 queries; 1024 of the
+  // shorter ones of 64 keys).  There are then at most as many pieces beyond one a tile as fill it, and none longer than what each of those
+  // has to do on average.  With enough tiles the most expensive first are balance enough: 24 documents in 8192 tokens, 16 / 8 heads of
+  // 128, dq 80 us without, 79 with pieces, dk and dv 75 and 84, and each list to join costs its launch.  With few they are most of the speed, in us
+  // without / with: 1 x 10612 tokens, 2 heads of 128, forward 261 / 109, dq 394 / 168, dk and dv 308 / 200; 3 sequences in 8192, 16 heads of
+  // 64 on one, dk and dv 1080 / 194.  None where no tile is as long as two pieces.
+  const int64_t tq = Tq / 128 + n_seq, tk = Tk / kTok + n_seq;
+  const int64_t long_q = (Tk + kTok - 1) / kTok, long_k = n_q / n_kv * ((Tq + kTok - 1) / kTok);
+  auto extra = [](int64_t full_tiles, int64_t enough, int64_t slots, int64_t heads, int64_t tiles, int64_t longest) {
+    if (full_tiles * heads >= enough) return 0;
+    return static_cast<int>(std::min((slots + heads - 1) / heads, tiles * ((longest + kLeastPiece - 1) / kLeastPiece - 1)));
+  };
+  z.extra_q = extra(Tq / 128, 768, 512, n_q, tq, long_q);
+  z.extra_k = extra(Tk / kTok, 1024, 1024, n_kv, tk, long_k);
+  z.max_q = tq + z.extra_q;
+  z.max_k = tk + z.extra_k;
+  int64_t at = z.q_at + kItemWords * z.max_q;
+  auto take = [&](int64_t words) {
+    const int64_t r = at;
+    at += words;
+    return static_cast<int>(r);
+  };
+  z.k_at = take(kItemWords * z.max_k);
+  z.join_at[0] = take(8 * std::max(1, z.extra_q));
+  z.join_at[1] = take(8 * std::max(1, z.extra_k));
+  z.words = at;
   return z;
+}
+
+// float32 sums of pieces: of the forward; of the backward behind delta, first dq's, then in the same place those of dk and dv
+int64_t masked_fwd_floats(const PlanSizes& z, const MaskedDims& d, bool single) {
+  if (single) return z.max_q * d.n_q * (d.dh + kPartExtra);
+  return (int64_t)2 * z.extra_q * d.n_q * 128 * (d.dh + kPartExtra);
+}
+int64_t masked_bwd_floats(const PlanSizes& z, const MaskedDims& d) {
+  return round_up(d.n_q * d.Tq, 64) + std::max((int64_t)2 * z.extra_q * d.n_q * 128 * d.dh, (int64_t)2 * z.extra_k * d.n_kv * 128 * d.dh);
 }
 
 hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int* k_start, const int* k_len, const int* prefix, const PlanTag& tag,
@@ -1068,7 +1201,7 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
 #define FAAR_MF2(H, M)                                                                                                              \
   do {                                                                                                                              \
     if (single) hipLaunchKernelGGL((k_masked_token<H, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, part);         \
-    else hipLaunchKernelGGL((k_masked_fwd<H, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, o_low);                 \
+    else hipLaunchKernelGGL((k_masked_fwd<H, M>), grid, dim3(256), 0, st, Q, K, V, plan, tag, z, d, O, lse, o_low, part);           \
   } while (0)
 #define FAAR_MF(M) \
   do { if (d.dh <= 64) FAAR_MF2(Heads64, M); else if (d.dh <= 96) FAAR_MF2(Heads96, M); else FAAR_MF2(Heads128, M); } while (0)
@@ -1081,37 +1214,24 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
 #undef FAAR_MF
 #undef FAAR_MF2
   if (hipError_t e = hipGetLastError()) return e;
+  if (!single && z.extra_q > 0)
+    hipLaunchKernelGGL(k_masked_join_fwd, dim3(static_cast<unsigned>(z.extra_q * d.n_q)), dim3(kJoinThreads), 0, st, plan, tag, z, d, part, O, lse, o_low);
   if (single && d.Tk > kPieceKeys)                     // no more keys than a block: no sequence has a second piece
     hipLaunchKernelGGL(k_masked_join, dim3(static_cast<unsigned>(d.Tq * d.n_q)), dim3(128), 0, st, plan, tag, z, d, part, O, lse);
   return hipGetLastError();
 }
 
-// Into how many parts the query heads of a key / value head are dealt: where few key / value heads leave fewer workgroups of 64 keys than
-// fill the device a few times over, equal parts that make them 2048 at most.  dk and dv in us with one part / up to 1024 / 2048 / 4096
-// workgroups: 3 sequences in 8192 tokens, 16 heads of 64 on one 1080 / 311 / 207 / 163 (and 8 to 25 for adding up), of 128 on two 747 / 421
-// / 281 / 292; in 7001, of 64 on four 251 / 146 / 120 / 120; in 2048, of 128 on one 383 / 39 / 40 / 41.
-int masked_bwd_parts(const PlanSizes& z, int64_t n_q, int64_t n_kv) {
-  const int64_t rep = n_q / n_kv, groups = z.max_k * n_kv;
-  int64_t parts = 1;
-  for (int64_t p = 2; p <= rep && groups * p <= 2048; ++p)
-    if (rep % p == 0) parts = p;
-  return static_cast<int>(parts);
-}
-int64_t masked_bwd_floats(const PlanSizes& z, int64_t n_q, int64_t n_kv, int64_t dh, int64_t Tq, int64_t Tk) {
-  const int64_t parts = masked_bwd_parts(z, n_q, n_kv);
-  return round_up(n_q * Tq, 64) + (parts > 1 ? parts * 2 * Tk * n_kv * dh : 0);
-}
-
 hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
                              const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* ws, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st) {
-  const int parts = masked_bwd_parts(z, d.n_q, d.n_kv);
   float *delta = ws, *part = ws + round_up(d.n_q * d.Tq, 64);
-  const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv * parts));
-#define FAAR_MB2(H, C, B)                                                                                                             \
-  do {                                                                                                                                \
-    hipLaunchKernelGGL((k_masked_bwd_dq<H, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ);     \
-    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV, parts, part); \
+  const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv));
+#define FAAR_MB2(H, C, B)                                                                                                               \
+  do {                                                                                                                                  \
+    hipLaunchKernelGGL((k_masked_bwd_dq<H, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ, part); \
+    if (z.extra_q > 0)                                                                                                                  \
+      hipLaunchKernelGGL(k_masked_join_grad<0>, dim3(static_cast<unsigned>(z.extra_q * d.n_q)), dim3(kJoinThreads), 0, st, plan, tag, z, d, part, dQ, dQ); \
+    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV, part);      \
   } while (0)
 #define FAAR_MB(C, B) \
   do { if (d.dh <= 64) FAAR_MB2(Heads64, C, B); else if (d.dh <= 96) FAAR_MB2(Heads96, C, B); else FAAR_MB2(Heads128, C, B); } while (0)
@@ -1120,8 +1240,8 @@ hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K,
 #undef FAAR_MB
 #undef FAAR_MB2
   if (hipError_t e = hipGetLastError()) return e;
-  if (parts > 1)
-    hipLaunchKernelGGL(k_masked_join_dkv, dim3(static_cast<unsigned>(z.max_k), 2, 4), dim3(256), 0, st, plan, tag, z, d, part, parts, dK, dV);
+  if (z.extra_k > 0)
+    hipLaunchKernelGGL(k_masked_join_grad<1>, dim3(static_cast<unsigned>(z.extra_k * d.n_kv)), dim3(kJoinThreads), 0, st, plan, tag, z, d, part, dK, dV);
   return hipGetLastError();
 }
 

@@ -177,45 +177,79 @@ CASES = {
     "many_128": Case(packed([130, 1, 200, 128, 65, 250] * 2), 32, 4, 128, slopes=True),
     "many_whole_96": Case(packed([130, 33, 200, 129] * 3), 32, 32, 88, causal=False),
     "many_windows": Case(packed([300] * 5, prefix=40), 32, 2, 72, window=70, cap=90.0, slopes=True, fused=True),
-    # a workgroup of dk and dv takes both query heads of a key / value head; two of its four; (above: one)
+    # few and many heads and keys beside one another: tiles in pieces, whole, and of many query heads
+    "one_head_long": Case(packed([1300, 700]), 1, 1, 128, cap=20.0),
+    "few_queries_long_keys": Case([(0, 3, 0, 1900, 0), (3, 40, 1900, 700, 0), (43, 0, 2600, 10, 0)], 4, 1, 64, same=False, slopes=True),
     "pairs_of_heads": Case(packed([130, 64, 200, 129, 65] * 3), 64, 32, 32, cap=5.0),
     "quads_of_heads": Case(packed([130, 64, 200, 129, 65] * 3), 64, 16, 24, window=100),
     "long": Case(packed([1500, 37]), 1, 1, 64, cap=30.0),
 }
 
 
+def plan_layout(Tq, Tk, n, n_q, n_kv):
+    """Where a plan has its lists: (places, bounds) of query items, key items, tiles of queries and of keys in pieces."""
+    ceil = lambda x, y: -(-x // y)
+    tq, tk = Tq // 128 + n, Tk // 64 + n
+    eq = 0 if Tq // 128 * n_q >= 768 else min(ceil(512, n_q), tq * (ceil(ceil(Tk, 64), 8) - 1))
+    ek = 0 if Tk // 64 * n_kv >= 1024 else min(ceil(1024, n_kv), tk * (ceil(n_q // n_kv * ceil(Tq, 64), 8) - 1))
+    q_at, k_at = 16, 16 + 16 * (tq + eq)
+    jq = k_at + 16 * (tk + ek)
+    return (q_at, k_at, jq, jq + 8 * max(1, eq)), (tq + eq, tk + ek, eq, ek)
+
+
 @pytest.mark.gpu
 def test_plan_lists_every_tile_once():
-    """Tiles cover the rows of every sequence once, lie inside it, come with the blocks that its masks leave, the most expensive first."""
+    """Tiles cover the rows of every sequence once and lie inside it; their pieces cover the blocks that the masks leave once; what is in
+    pieces has its own places; the most expensive come first."""
+    in_pieces = set()
     for name, c in CASES.items():
         a, _ = c.device()
         plan = faar.faar_attention_plan(a).view(torch.int32).cpu().numpy()
-        bad, no_bwd, nq, nk = plan[8:12]
+        bad, no_bwd, nq, nk, jq, jk = plan[8:14]
         assert (bad, no_bwd) == (0, 0), name
-        q_at, max_q = 16, c.Tq // 128 + len(c.seqs)
-        k_at = q_at + 8 * max_q
-        qi, ki = plan[q_at:q_at + 8 * nq].reshape(-1, 8), plan[k_at:k_at + 8 * nk].reshape(-1, 8)
-        assert nq == sum(-(-s[1] // 128) for s in c.seqs) <= max_q and nk == sum(-(-s[3] // 64) for s in c.seqs) <= c.Tk // 64 + len(c.seqs)
-        seen = np.zeros(c.Tq, int)
-        for row0, rows, pos, ks, kl, pre, b0, b1 in qi:
-            qs, ql, ks_, kl_, pre_ = next(s for s in c.seqs if s[0] <= row0 < s[0] + s[1])
-            assert (row0 - qs) % 128 == 0 and 1 <= rows <= 128 and row0 + rows <= qs + ql and (ks, kl) == (ks_, kl_) and pre == min(pre_, kl)
-            assert pos == kl - ql + row0 - qs
-            ok = bo.allowed_keys(ql, kl, c.causal, pre_, c.window)[row0 - qs:row0 - qs + rows].any(axis=0)
-            j = np.flatnonzero(ok)
-            assert 0 <= b0 <= b1 <= -(-kl // 64) and (j.size == 0 or (b0 <= j[0] // 64 and j[-1] // 64 < b1)), (name, b0, b1)
-            seen[row0:row0 + rows] += 1
-        assert np.array_equal(seen, c.q_rows.astype(int)), name
-        costs = qi[:, 7] - qi[:, 6]
-        most = max(-(-s[3] // 64) for s in c.seqs) + 1
-        bucket = costs.astype(np.int64) * 128 // most
-        assert (np.diff(bucket) <= 0).all(), name
-        seen = np.zeros(c.Tk, int)
-        for row0, rows, k0, qs, ql, off, pre, _ in ki:
-            qs_, ql_, ks, kl, pre_ = next(s for s in c.seqs if s[2] <= row0 < s[2] + s[3])
-            assert k0 == row0 - ks and k0 % 64 == 0 and 1 <= rows <= 64 and k0 + rows <= kl and (qs, ql, off, pre) == (qs_, ql_, kl - ql, min(pre_, kl))
-            seen[row0:row0 + rows] += 1
-        assert np.array_equal(seen, c.k_rows.astype(int)), name
+        at, most = plan_layout(c.Tq, c.Tk, len(c.seqs), c.n_q, c.n_kv)
+        assert nq <= most[0] and nk <= most[1] and jq <= most[2] and jk <= most[3], name
+        for kind, (n_items, n_joins) in enumerate(((nq, jq), (nk, jk))):
+            items = plan[at[kind]:at[kind] + 16 * n_items].reshape(-1, 16)
+            joins = {int(w[0]): w for w in plan[at[2 + kind]:at[2 + kind] + 8 * n_joins].reshape(-1, 8)}
+            assert len(joins) == n_joins
+            tiles, used = {}, []
+            for w in items:
+                tiles.setdefault(int(w[0]), []).append(w)
+            rows_seen = np.zeros(c.Tk if kind else c.Tq, int)
+            for row0, pieces in tiles.items():
+                pieces.sort(key=lambda w: w[7 if kind else 6])
+                w = pieces[0]
+                qs, ql, ks, kl, pre = next(s for s in c.seqs if s[2 * kind] <= row0 < s[2 * kind] + s[2 * kind + 1])
+                start, length, size = (ks, kl, 64) if kind else (qs, ql, 128)
+                rows = int(w[1])
+                assert (row0 - start) % size == 0 and rows == min(size, start + length - row0), name
+                rows_seen[row0:row0 + rows] += 1
+                ok = bo.allowed_keys(ql, kl, c.causal, pre, c.window)
+                if kind:
+                    assert tuple(w[2:7]) == (row0 - ks, qs, ql, kl - ql, min(pre, kl)), name
+                    i = np.flatnonzero(ok[:, row0 - ks:row0 - ks + rows].any(axis=1))
+                    want = c.n_q // c.n_kv * (i[-1] // 64 + 1 - i[0] // 64) if i.size else 0
+                    spans, slots = [(int(p[7]), int(p[8])) for p in pieces], [int(p[9]) for p in pieces]
+                    assert spans[0][0] == 0 and spans[-1][1] == want, (name, spans, want)
+                else:
+                    assert tuple(w[2:6]) == (kl - ql + row0 - qs, ks, kl, min(pre, kl)), name
+                    j = np.flatnonzero(ok[row0 - qs:row0 - qs + rows].any(axis=0))
+                    spans, slots = [(int(p[6]), int(p[7])) for p in pieces], [int(p[8]) for p in pieces]
+                    if j.size:
+                        assert spans[0][0] == j[0] // 64 and spans[-1][1] == j[-1] // 64 + 1, (name, spans)
+                assert all(x[1] == y[0] and x[0] < x[1] for x, y in zip(spans, spans[1:])), (name, spans)
+                if len(pieces) == 1:
+                    assert slots == [-1] and row0 not in joins
+                else:
+                    in_pieces.add(kind)
+                    assert tuple(joins[row0][1:4]) == (rows, slots[0], len(pieces)) and slots == list(range(slots[0], slots[0] + len(pieces)))
+                    used += slots
+            assert np.array_equal(rows_seen, (c.k_rows if kind else c.q_rows).astype(int)), name
+            assert sorted(used) == list(range(len(used))) and len(used) <= 2 * most[2 + kind], name
+            costs = (items[:, 8] - items[:, 7]) if kind else (items[:, 7] - items[:, 6])
+            assert len(costs) == 0 or (np.diff(costs) <= costs.max() // 64 + 1).all(), name
+    assert in_pieces == {0, 1}
 
 
 @pytest.mark.gpu
@@ -289,10 +323,10 @@ def test_single_tokens(name):
     cols = n_kv * -(-(n_q // n_kv) // 32)
     target, pieces = -(-512 // cols), int(words[10])
     assert pieces <= n + target
-    items, first = words[16:16 + 8 * pieces].reshape(-1, 8), 0
+    items, first = words[16:16 + 16 * pieces].reshape(-1, 16), 0
     for b, L in enumerate(lens):                           # the pieces of a cache follow one another and end with it
         mine = items[items[:, 0] == b]
-        assert len(mine) == mine[0, 4] and words[16 + 8 * (n + target) + 2 * b] == first
+        assert len(mine) == mine[0, 4] and words[16 + 16 * (n + target) + 2 * b] == first
         at = b * cap_rows + (max(0, L - window) if window else 0)
         for _, row, keys, gap, *_ in mine:
             assert row == at and keys >= 0 and gap == L - 1 - (row - b * cap_rows)
