@@ -108,6 +108,7 @@ __device__ __forceinline__ Seen queries_of(int j, int q_len, int off, int prefix
 }
 
 // ---- the plan -----------------------------------------------------------------------------------------------------------------
+constexpr int kSmallCaches = 4 * kPieceKeys;   // single tokens: rows of all caches
 constexpr int kJoinThreads = 1024;     // a workgroup that adds up pieces
 constexpr int kPlanThreads = 1024, kBuckets = 128, kLeastPiece = 8;
 
@@ -159,7 +160,7 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
 
   if (single) {
     // pieces of whole blocks, as equal as the total over the sequences allows; every sequence has one at least
-    const int per = static_cast<int>(max(1ull, (sums[0] + z.target - 1) / z.target));
+    const int per = z.target == 0 ? 1 << 20 : static_cast<int>(max(1ull, (sums[0] + z.target - 1) / z.target));
     for (int b0 = 0; b0 < n_seq; b0 += kPlanThreads) {
       const int b = b0 + tid;
       const int blocks = b < n_seq ? blocks_of(b) : 0, n = b < n_seq ? max(1, (blocks + per - 1) / per) : 0;
@@ -994,7 +995,8 @@ k_masked_join_grad(const int* __restrict__ plan, PlanTag tag, PlanSizes z, Maske
 
 // ---- one token a sequence ---------------------------------------------------------------------------------------------------------
 // A workgroup takes one piece of a sequence's keys for one key / value head and up to 32 of its query heads, which are the columns of
-// the products: blocks of 128 keys, 32 a wavefront, two stages.  The four wavefronts' sums meet through LDS; a sequence of one piece is
+// the products: blocks of 128 keys, 32 a wavefront, two stages (four, which leave room for one workgroup a unit with heads
+// of 64, are slower: 64 caches of up to 8192 keys, 8 heads, 131 -> 188 us).  The four wavefronts' sums meet through LDS; a sequence of one piece is
 // done, others leave (O, maximum, denominator) of the piece in the workspace for k_masked_join.  Bound by the one pass over the cache.
 template <class H, int kMode>
 __global__ void __launch_bounds__(256, 1)
@@ -1109,25 +1111,43 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
   }
 }
 
-// the pieces of a sequence, one query head a workgroup, in their order
+// The pieces of a sequence, one query head a workgroup, in their order, eight at a time: one round trip to memory brings the plan's words,
+// the next all that eight pieces left
 __global__ void __launch_bounds__(128)
 k_masked_join(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d, const float* __restrict__ part, bf16_t* __restrict__ O,
               float* __restrict__ lse) {
   const int seq = blockIdx.x / d.n_q, head = blockIdx.x % d.n_q;
-  const PlanWords w(plan, z.q_at, 0, threadIdx.x & 63);
-  if (!w.is(tag, false)) return;                       // answered by the kernel before
-  const int first = plan[z.seq_at + 2 * seq], pieces = plan[z.seq_at + 2 * seq + 1];
-  if (pieces == 1) return;
+  const PlanLook<2> w(plan, z.seq_at, seq, threadIdx.x & 63);
+  const int first = w.item(0), pieces = w.item(1);
+  if (!w.is(tag, false) || pieces == 1) return;        // a wrong plan: answered by the kernel before
   const int64_t step = (int64_t)d.n_q * (d.dh + kPartExtra);
   const float* p = part + first * step + head * (d.dh + kPartExtra);
-  float m = kLowest, l = 0.0f, r = 0.0f, x = 0.0f;
-  for (int i = 0; i < pieces; ++i) m = fmaxf(m, p[i * step + d.dh]);
   const bool on = threadIdx.x < d.dh;
-  for (int i = 0; i < pieces; ++i) {
-    const float f = fast_exp2(p[i * step + d.dh] - m);
-    l += p[i * step + d.dh + 1] * f;
-    r += p[i * step + d.dh + 2] * f;
-    if (on) x += p[i * step + threadIdx.x] * f;
+  float m = kLowest, l = 0.0f, r = 0.0f, x = 0.0f;
+  for (int i0 = 0; i0 < pieces; i0 += 8) {
+    float mi[8], li[8], ri[8], xi[8], top = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float* q = p + min(i0 + i, pieces - 1) * step;                 // the last one again, with weight 0
+      mi[i] = i0 + i < pieces ? q[d.dh] : kLowest;
+      li[i] = q[d.dh + 1];
+      ri[i] = q[d.dh + 2];
+      xi[i] = q[on ? threadIdx.x : 0];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, mi[i]);
+    const float f = fast_exp2(m - top);
+    l *= f;
+    r *= f;
+    x *= f;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float g = i0 + i < pieces ? fast_exp2(mi[i] - m) : 0.0f;
+      l = fmaf(li[i], g, l);
+      r = fmaf(ri[i], g, r);
+      x = fmaf(xi[i], g, x);
+    }
   }
   if (on) O[(int64_t)seq * d.ldo + head * d.dh + threadIdx.x] = static_cast<bf16_t>(f32_to_bf16(r > 0.0f ? x / r : 0.0f));
   if (lse && threadIdx.x == 0) lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
@@ -1140,7 +1160,9 @@ PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_
   z.q_at = 16;
   if (single) {
     const int64_t cols = n_kv * ((n_q / n_kv + 31) / 32);
-    z.target = static_cast<int>((512 + cols - 1) / cols);
+    // pieces: about 512 workgroups; small caches in one piece each, since joining costs as much as walking four blocks of
+    // keys (700 keys, 8 heads of 64, on the device: six pieces and their join 5.5 + 3.2 us, whole 10.3)
+    z.target = Tk <= kSmallCaches ? 0 : static_cast<int>((512 + cols - 1) / cols);
     z.max_q = n_seq + z.target;
     z.seq_at = static_cast<int>(z.q_at + kItemWords * z.max_q);
     z.words = z.seq_at + 2 * n_seq;
@@ -1216,7 +1238,7 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
   if (hipError_t e = hipGetLastError()) return e;
   if (!single && z.extra_q > 0)
     hipLaunchKernelGGL(k_masked_join_fwd, dim3(static_cast<unsigned>(z.extra_q * d.n_q)), dim3(kJoinThreads), 0, st, plan, tag, z, d, part, O, lse, o_low);
-  if (single && d.Tk > kPieceKeys)                     // no more keys than a block: no sequence has a second piece
+  if (single && z.target > 0)
     hipLaunchKernelGGL(k_masked_join, dim3(static_cast<unsigned>(d.Tq * d.n_q)), dim3(128), 0, st, plan, tag, z, d, part, O, lse);
   return hipGetLastError();
 }

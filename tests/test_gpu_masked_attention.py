@@ -291,6 +291,7 @@ TOKENS = {  # lengths of the caches, capacity, n_q, n_kv, dh, window, cap, slope
     "many_heads_share": ([40, 333], 384, 80, 2, 64, 0, 0.0, False),
     "long_alone": ([9001], 9100, 2, 1, 128, 0, 30.0, False),
     "heads_of_96": ([40, 300, 128], 320, 4, 2, 96, 0, 10.0, False),
+    "one_piece_each": ([170, 1, 0], 170, 8, 8, 64, 0, 0.0, True),
     "small_caches": ([40, 3, 17], 40, 4, 1, 24, 0, 0.0, False),
     "high_cap": ([300, 200], 300, 2, 2, 128, 0, 100.0, False),
 }
@@ -321,7 +322,7 @@ def test_single_tokens(name):
     plan = faar.faar_attention_plan(a)
     words = plan.view(torch.int32).cpu().numpy()
     cols = n_kv * -(-(n_q // n_kv) // 32)
-    target, pieces = -(-512 // cols), int(words[10])
+    target, pieces = 0 if n * cap_rows <= 512 else -(-512 // cols), int(words[10])
     assert pieces <= n + target
     items, first = words[16:16 + 16 * pieces].reshape(-1, 16), 0
     for b, L in enumerate(lens):                           # the pieces of a cache follow one another and end with it
