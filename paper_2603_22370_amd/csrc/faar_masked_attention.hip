@@ -346,7 +346,7 @@ __device__ __forceinline__ float add_pair(uint32_t w, float a) {
 // `len` keys from 0 on are seen (masked); gap: distance of the lane's first key from its query.
 template <class H, int kMode, int NT>
 __device__ __forceinline__ void masked_block(MaskedState<H>& st, uint32_t k_lds, uint32_t v_lds, uint32_t ra, uint32_t ca, const Scores& sc,
-                                             int h0, bool masked, int first, int len, float gap) {
+                                             int h0, bool masked, int first, int len, float gap, bool raw) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   f32x16 s[NT];            // rows = keys, column = query
@@ -417,9 +417,14 @@ __device__ __forceinline__ void masked_block(MaskedState<H>& st, uint32_t k_lds,
       else if constexpr (kMode == kBounded) p = fast_exp2(s[kt][v]);
       else p = fast_exp2(s[kt][v] - st.mc);
       s[kt][v] = p;
-      ps += p;
     }
-  st.l += ps;
+  if (raw) {
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) ps += s[kt][v];
+    st.l += ps;
+  }
   Frag p[NT][2];
 #pragma unroll
   for (int kt = 0; kt < NT; ++kt) {
@@ -549,7 +554,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
     if (mine <= 0 || k0 >= sb.hi || k0 + kTok <= sa.lo) continue;
     const float gap = static_cast<float>(p - k0 - 4 * hi);
     masked_block<H, kMode, 2>(st, k_lds, v_lds, ra, ca, sc, 0, !(k0 >= sb.lo && k0 + kTok <= sa.hi), k0 + 4 * hi - seen.lo,
-                               max(0, seen.hi - seen.lo), gap);
+                               max(0, seen.hi - seen.lo), gap, lse != nullptr);
   }
   __syncthreads();                                     // the tiles have been read: their place is free
   if (mine <= 0) return;
@@ -1052,7 +1057,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
     const int j0 = blk * kPieceKeys + 32 * wave;
     if (j0 >= keys) continue;
     const float gap = static_cast<float>(gap0 - j0 - 4 * hi);
-    masked_block<H, kMode, 1>(st, k_lds, v_lds, ra, ca, sc, wave & 1, j0 + 32 > keys, j0 + 4 * hi, keys, gap);
+    masked_block<H, kMode, 1>(st, k_lds, v_lds, ra, ca, sc, wave & 1, j0 + 32 > keys, j0 + 4 * hi, keys, gap, lse != nullptr);
   }
   // the wavefronts' sums on a common maximum
   const float lt = half_sum(st.l), lr = half_sum(st.lr);
