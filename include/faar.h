@@ -667,7 +667,8 @@ int faar_rope_axes(const void* q, int64_t ldq, int64_t n_q, const void* k, int64
  * Softmax attention over ragged sequences under masks, with capped or biased scores.  Sequence b is q_len[b] rows of q from row
  * q_start[b] on and k_len[b] rows of k and v from row k_start[b] on; its queries are the LAST positions: query i stands at position
  * p = k_len[b] - q_len[b] + i, key j at position j.  Rows may lie packed (start = sum of the lengths before), padded or in a cache
- * (start = b * capacity); rows of no sequence are neither read nor written.  For head h and its key / value head h / (n_q / n_kv):
+ * (start = b * capacity); rows of no sequence are neither read nor written, whatever they hold.  (Rows of a sequence are finite: a key
+ * that a query does not see has probability 0, by which its values are multiplied.)  For head h and its key / value head h / (n_q / n_kv):
  *
  *   z = scale q.k;   s = cap tanh(z / cap) - slopes[h] |p - j|   (cap 0: s = z - ...; slopes NULL: no bias)
  *   p sees j iff  |p - j| < window (where window > 0)  and, with FAAR_ATTENTION_CAUSAL, j <= p or j < prefix[b]

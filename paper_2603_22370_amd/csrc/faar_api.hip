@@ -1017,7 +1017,7 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
   c.z = attention_plan_sizes(a->n_seq, a->Tq, a->Tk, a->n_q, a->n_kv, c.single);
   // the largest grids: work items x heads, and for single tokens one query head of a sequence each
   if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * 2 * a->n_kv > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
-  const int window = a->window > kMaxRows ? 0 : static_cast<int>(a->window);     // wider than any sequence: none
+  const int window = a->window >= kMaxRows ? 0 : static_cast<int>(a->window);    // no two positions are that far apart: none
   const int tag[kPlanTagWords] = {0x5A11FAA3, static_cast<int>(a->flags) | (c.single ? 2 : 0), static_cast<int>(a->n_seq), static_cast<int>(a->Tq),
                                   static_cast<int>(a->Tk), window, static_cast<int>(a->n_q), static_cast<int>(a->n_kv)};
   for (int i = 0; i < kPlanTagWords; ++i) c.tag.w[i] = tag[i];
