@@ -55,17 +55,19 @@ template <int DH>
 __device__ __forceinline__ void copy_tile(const bf16_t* __restrict__ src, int64_t row0, int valid, int64_t ld, int64_t col0, int dh,
                                           uint32_t lane_offset, uint32_t tile, int wave, int tid) {
   typedef Tile<DH> Tl;
-  asm volatile("" : "+v"(tid));        // addresses are formed here, where few blocks come by, and not kept in registers throughout
+  // the address of the tile, the same for all lanes, in scalar registers: said lane by lane, where the compiler does not see it
+  const uint64_t at = reinterpret_cast<uint64_t>(src + row0 * ld + col0);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+  const bf16_t* base = reinterpret_cast<const bf16_t*>(static_cast<uint64_t>(hi) << 32 | lo);
+  if (valid >= kTok && dh == DH) {
+    Tl::copy(base, 0, kTok, ld, 0, lane_offset, tile, wave);
+    return;
+  }
+  asm volatile("" : "+v"(tid));        // lanes' own addresses are formed here, where few blocks come by, and not kept in registers throughout
   const int r = tid / Tl::CPR, col = ((tid % Tl::CPR) ^ Tl::key(r)) * 8;
   if (col >= dh) return;               // these lanes copy nothing
   if (valid >= kTok) {
-    // addresses that are the same for all lanes go in scalar registers, said lane by lane where the compiler does not see it
-#pragma unroll
-    for (int j = 0; j < Tl::COPIES; ++j) {
-      const uint64_t at = reinterpret_cast<uint64_t>(src + (row0 + j * (256 / Tl::CPR)) * ld + col0);
-      const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
-      dma16(reinterpret_cast<const void*>(static_cast<uint64_t>(hi) << 32 | lo), lane_offset, __builtin_amdgcn_readfirstlane(tile + 4096u * j + 1024u * wave));
-    }
+    Tl::copy(base, 0, kTok, ld, 0, lane_offset, tile, wave);
     return;
   }
 #pragma unroll
