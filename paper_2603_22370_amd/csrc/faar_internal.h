@@ -199,7 +199,7 @@ struct PlanSizes { int q_at, k_at, seq_at, join_at[2], target, extra_q, extra_k;
 struct MaskedDims {
   int n_q, n_kv, dh;
   int64_t Tq, Tk, ldq, ldk, ldv, ldo;   // rows; elements between rows
-  float scale, c, cap_a, cap_b, ref;    // c = scale log2 e; cap_a = cap log2 e (0: none), cap_b = 2 scale log2 e / cap; ref: see launch_masked_fwd
+  float grad_scale, c, cap_a, cap_b, ref;    // of dq and dk: scale, capped 4 scale; c = scale log2 e; cap_a = cap log2 e (0: none), cap_b = 2 scale log2 e / cap; ref: see launch_masked_fwd
   const float* slopes;                  // nullable [n_q]
 };
 PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, bool single);
@@ -210,7 +210,7 @@ constexpr int kPartExtra = 3;
 // o_low: nullable [Tq][n_q * dh], the 8 bits behind each bf16 of O (forward out, not with single tokens; backward in)
 hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
                              const MaskedDims& d, bool single, bf16_t* O, float* lse, uint8_t* o_low, float* part, hipStream_t st);
-// ws: masked_bwd_floats (delta [n_q][Tq], then sums of pieces)
+// ws: masked_bwd_floats (delta and shift [n_q][Tq], then sums of pieces)
 int64_t masked_fwd_floats(const PlanSizes& z, const MaskedDims& d, bool single);
 int64_t masked_bwd_floats(const PlanSizes& z, const MaskedDims& d);
 hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,

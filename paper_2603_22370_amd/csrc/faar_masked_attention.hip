@@ -623,16 +623,18 @@ k_masked_join_fwd(const int* __restrict__ plan, PlanTag tag, PlanSizes z, Masked
 }
 
 // ---- backward: dq ---------------------------------------------------------------------------------------------------------------
-// x: q.k of an element -> its probability, and what the cap leaves of a gradient (1 - tanh^2)
+// x: q.k of an element -> its probability, with `shift` what a query's scores are shifted by (in units of log 2; capped: the cap less
+// lse, else -lse); and a quarter of what the cap leaves of a gradient: with r = (1 - tanh) / 2, 1 - tanh^2 = 4 (r - r^2).  The 4 is in
+// d.grad_scale.
 template <bool kCap, bool kBias>
-__device__ __forceinline__ float prob_of(float x, const Scores& sc, float lse2, float gap, float& slack) {
+__device__ __forceinline__ float prob_of(float x, const Scores& sc, float shift, float gap, float& slack) {
   float y;
   if constexpr (kCap) {
     const float r = cap_half(sc, x);
-    slack = 4.0f * r * (1.0f - r);
-    y = fmaf(-2.0f * sc.a, r, sc.a) - lse2;
+    slack = fmaf(-r, r, r);
+    y = fmaf(-2.0f * sc.a, r, shift);
   } else {
-    y = fmaf(x, sc.c, -lse2);
+    y = fmaf(x, sc.c, shift);
   }
   if constexpr (kBias) y = fmaf(-sc.slope, fabsf(gap), y);
   return fast_exp2(y);
@@ -641,7 +643,7 @@ __device__ __forceinline__ float prob_of(float x, const Scores& sc, float lse2, 
 // 32 keys (half kt of the tiles).  The operands from LDS pass through a ring of kRing, each requested kRing - 1 matrix instructions
 // ahead, as in the dk / dv kernel, and for its reason: with all of them requested at once registers run out.
 template <class H, bool kCap, bool kBias>
-__device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x8 (&qf)[H::KS], const bf16x8 (&dof)[H::KS], float lse2,
+__device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x8 (&qf)[H::KS], const bf16x8 (&dof)[H::KS], float shift,
                                                float dl, uint32_t k_rows, uint32_t v_rows, uint32_t k_cols, const Scores& sc, bool masked,
                                                int first, int len, float gap) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
@@ -663,7 +665,7 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
   for (int v = 0; v < 16; ++v) {
     const int j = 8 * (v / 4) + v % 4;
     float slack = 1.0f;
-    float p = prob_of<kCap, kBias>(s[v], sc, lse2, gap - static_cast<float>(j), slack);
+    float p = prob_of<kCap, kBias>(s[v], sc, shift, gap - static_cast<float>(j), slack);
     dp[v] = p * (dp[v] - dl);
     if constexpr (kCap) dp[v] *= slack;
   }
@@ -714,7 +716,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
   const int64_t t0 = (int64_t)row0 + 32 * wave + n;
 
   bf16x8 qf[KS], dof[KS];
-  float lse2 = 0.0f, dl = 0.0f;
+  float shift = 0.0f, dl = 0.0f;
   f32x16 acc[DT];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
@@ -732,8 +734,11 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
   }
   dl = half_sum(dl);
   if (live) {
-    lse2 = lse[(int64_t)head * d.Tq + t0] * kLog2e;
-    if (hi == 0) delta[(int64_t)head * d.Tq + t0] = dl;
+    shift = (kCap ? sc.a : 0.0f) - lse[(int64_t)head * d.Tq + t0] * kLog2e;
+    if (hi == 0) {
+      delta[(int64_t)head * d.Tq + t0] = dl;
+      delta[((int64_t)d.n_q + head) * d.Tq + t0] = shift;
+    }
   }
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
@@ -760,7 +765,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
 #pragma unroll 1
     for (int kt = 0; kt < 2; ++kt) {
       const uint32_t half = kt * (32 * DH * 2);
-      masked_dq_tile<H, kCap, kBias>(acc, qf, dof, lse2, dl, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
+      masked_dq_tile<H, kCap, kBias>(acc, qf, dof, shift, dl, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
                                       gap - 32 * kt);
     }
   }
@@ -777,7 +782,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
     for (int j = 0; j < 4; ++j) {
       float x[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = acc[dt][4 * j + r] * d.scale;
+      for (int r = 0; r < 4; ++r) x[r] = acc[dt][4 * j + r] * d.grad_scale;
       RowStage<DH>::put(stage, lane, dt, j, x, false);
     }
   RowStage<DH>::flush(stage, lane, mine, d.dh, dQ + ((int64_t)row0 + 32 * wave) * d.ldq + head * d.dh, d.ldq, nullptr, 0);
@@ -788,7 +793,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
 // sees the lane's key, of `len`; gap: distance of the lane's key from the lane's first query.
 template <class H, bool kCap, bool kBias>
 __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv)[H::DT], const bf16x8 (&kf)[H::KS],
-                                                const bf16x8 (&vf)[H::KS], const float* lse_lds, const float* delta_lds, uint32_t q_rows,
+                                                const bf16x8 (&vf)[H::KS], const float* shift_lds, const float* delta_lds, uint32_t q_rows,
                                                 uint32_t q_cols, const Scores& sc, bool masked, int first, int len, float gap, int lane) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   constexpr uint32_t kDo = Tile<DH>::ELEMS * 2;     // the dO tile follows the q tile
@@ -809,13 +814,13 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int row = 8 * j + 4 * (lane >> 5);
-    const float4 l4 = *reinterpret_cast<const float4*>(lse_lds + row);
+    const float4 l4 = *reinterpret_cast<const float4*>(shift_lds + row);
     const float4 d4 = *reinterpret_cast<const float4*>(delta_lds + row);
     const float lr[4] = {l4.x, l4.y, l4.z, l4.w}, dr[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float slack = 1.0f;
-      float p = prob_of<kCap, kBias>(s[4 * j + r], sc, lr[r] * kLog2e, gap + static_cast<float>(8 * j + r), slack);
+      float p = prob_of<kCap, kBias>(s[4 * j + r], sc, lr[r], gap + static_cast<float>(8 * j + r), slack);
       s[4 * j + r] = p;
       float g = p * (dp[4 * j + r] - dr[r]);
       if constexpr (kCap) g *= slack;
@@ -850,12 +855,12 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
 template <class H, bool kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
-                 const float* __restrict__ lse, const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
+                 const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
                  bf16_t* __restrict__ dK, bf16_t* __restrict__ dV, float* __restrict__ part) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][Tl::ELEMS];   // [stage][q, dO]
-  __shared__ __attribute__((aligned(16))) float stats[2][2][kTok];         // [stage][lse, delta]
+  __shared__ __attribute__((aligned(16))) float stats[2][2][kTok];         // [stage][shift, delta]
   const int item = blockIdx.x / d.n_kv, kvh = blockIdx.x % d.n_kv;
   const PlanWords w(plan, z.k_at, item, threadIdx.x & 63);
   if (!w.is(tag, true)) {
@@ -900,7 +905,7 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
     copy_tile<DH>(Q, (int64_t)q_start + q0, q_len - q0, d.ldq, (int64_t)head * d.dh, d.dh, from_q, at, wave, tid);
     copy_tile<DH>(dO, (int64_t)q_start + q0, q_len - q0, d.ldo, (int64_t)head * d.dh, d.dh, from_o, at + Tl::ELEMS * 2, wave, tid);
     if (wave < 2)
-      dma4((wave == 0 ? lse : delta) + (int64_t)head * d.Tq + q_start + min(q0 + lane, q_len - 1),
+      dma4(delta + ((int64_t)(wave == 0 ? d.n_q : 0) + head) * d.Tq + q_start + min(q0 + lane, q_len - 1),
            __builtin_amdgcn_readfirstlane(lds_addr_of(stats[stage][wave])));
   };
   int head = kvh * heads, blk = first;
@@ -943,7 +948,7 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
   }
   __syncthreads();
   f32x16 sum[DT];
-  const float k = qw == 0 && slot < 0 ? d.scale : 1.0f;
+  const float k = qw == 0 && slot < 0 ? d.grad_scale : 1.0f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
     const f32x16 r = take[dt * 64];
@@ -994,7 +999,7 @@ k_masked_join_grad(const int* __restrict__ plan, PlanTag tag, PlanSizes z, Maske
     }
     if (set == 0)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) a[e] *= d.scale;
+      for (int e = 0; e < 8; ++e) a[e] *= d.grad_scale;
     const int64_t ld = kind == 0 ? d.ldq : set == 0 ? d.ldk : d.ldv;
     W8<bf16_t>::store((set == 0 ? A : B) + (row0 + row) * ld + head * d.dh + col, a);
   }
@@ -1210,7 +1215,7 @@ int64_t masked_fwd_floats(const PlanSizes& z, const MaskedDims& d, bool single) 
   return (int64_t)2 * z.extra_q * d.n_q * 128 * (d.dh + kPartExtra);
 }
 int64_t masked_bwd_floats(const PlanSizes& z, const MaskedDims& d) {
-  return round_up(d.n_q * d.Tq, 64) + std::max((int64_t)2 * z.extra_q * d.n_q * 128 * d.dh, (int64_t)2 * z.extra_k * d.n_kv * 128 * d.dh);
+  return round_up((int64_t)2 * d.n_q * d.Tq, 64) + std::max((int64_t)2 * z.extra_q * d.n_q * 128 * d.dh, (int64_t)2 * z.extra_k * d.n_kv * 128 * d.dh);
 }
 
 hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int* k_start, const int* k_len, const int* prefix, const PlanTag& tag,
@@ -1253,14 +1258,14 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
 hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const bf16_t* O, const uint8_t* o_low, const float* lse,
                              const int* plan, const PlanTag& tag, const PlanSizes& z, const MaskedDims& d, float* ws, bf16_t* dQ, bf16_t* dK,
                              bf16_t* dV, hipStream_t st) {
-  float *delta = ws, *part = ws + round_up(d.n_q * d.Tq, 64);
+  float *delta = ws, *part = ws + round_up(2 * d.n_q * d.Tq, 64);
   const dim3 gq(static_cast<unsigned>(z.max_q * d.n_q)), gk(static_cast<unsigned>(z.max_k * d.n_kv));
 #define FAAR_MB2(H, C, B)                                                                                                               \
   do {                                                                                                                                  \
     hipLaunchKernelGGL((k_masked_bwd_dq<H, C, B>), gq, dim3(256), 0, st, Q, K, V, dO, O, o_low, lse, plan, tag, z, d, delta, dQ, part); \
     if (z.extra_q > 0)                                                                                                                  \
       hipLaunchKernelGGL(k_masked_join_grad<0>, dim3(static_cast<unsigned>(z.extra_q * d.n_q)), dim3(kJoinThreads), 0, st, plan, tag, z, d, part, dQ, dQ); \
-    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, lse, delta, plan, tag, z, d, dK, dV, part);      \
+    hipLaunchKernelGGL((k_masked_bwd_dkv<H, C, B>), gk, dim3(256), 0, st, Q, K, V, dO, delta, plan, tag, z, d, dK, dV, part);           \
   } while (0)
 #define FAAR_MB(C, B) \
   do { if (d.dh <= 64) FAAR_MB2(Heads64, C, B); else if (d.dh <= 96) FAAR_MB2(Heads96, C, B); else FAAR_MB2(Heads128, C, B); } while (0)
