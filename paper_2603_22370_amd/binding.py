@@ -225,11 +225,12 @@ def _dev(*ts):
 _BF16, _F32 = torch.bfloat16, torch.float32
 
 
-def _raw_stream(t):
-    """The current stream, as an integer, on the tensor's device, which must be the current one: kernels are launched there."""
-    device = t.get_device()
-    if device != torch._C._cuda_getDevice():
-        raise ValueError("the tensors are on another device than the current one")
+def _raw_stream(*ts):
+    """The current stream, as an integer, on the current device, where kernels are launched and all of the tensors (or None) must be."""
+    device = torch._C._cuda_getDevice()
+    for t in ts:
+        if t is not None and t.get_device() != device:
+            raise ValueError("the tensors are on another device than the current one")
     return torch._C._cuda_getCurrentRawStream(device)
 
 
@@ -618,7 +619,7 @@ def faar_layernorm_fwd(x, g, b=None, eps=1e-5):
         _whole(b, _F32, D, where)
     h, mean, rstd = x.new_empty((T, D), dtype=_BF16), x.new_empty(T, dtype=_F32), x.new_empty(T, dtype=_F32)
     _check(lib().faar_layernorm_fwd(x.data_ptr(), _dt(x), T, D, g.data_ptr(), _at(b), eps, h.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                    _raw_stream(x)), where)
+                                    _raw_stream(x, g, b)), where)
     return h, mean, rstd
 
 
@@ -645,7 +646,7 @@ def faar_layernorm_bwd(dh1, x, g, mean, rstd, dh2=None, d_res=None, dh3=None, wa
     _dev(ws)
     _check(lib().faar_layernorm_bwd(dh1.data_ptr(), _at(dh2), _at(dh3), x.data_ptr(), _dt(x), T, D, g.data_ptr(), mean.data_ptr(),
                                     rstd.data_ptr(), _at(d_res), dx.data_ptr(), _at(dg), _at(db), _at(ws), 0 if ws is None else ws.numel(),
-                                    _raw_stream(x)), where)
+                                    _raw_stream(x, dh1, dh2, dh3, g, mean, rstd, d_res, ws)), where)
     return dx, dg, db
 
 
@@ -675,7 +676,7 @@ def faar_rope_axes(q, k, n_q, n_k, dh, pos, axis, freq, pairs=False, inverse=Fal
     fr = array.array("d", freq)
     _check(lib().faar_rope_axes(q.data_ptr(), ldq, n_q, _at(k), ldk, n_k, T, dh, 2 * half, pos.data_ptr(), n_axes, bytes(list(axis)),
                                 fr.buffer_info()[0], (FAAR_ROPE_PAIRS if pairs else 0) | (FAAR_ROPE_INVERSE if inverse else 0), yq.data_ptr(),
-                                ldyq, _at(yk), ldyk, _raw_stream(q)), where)
+                                ldyq, _at(yk), ldyk, _raw_stream(q, k, pos, yq, yk)), where)
     return yq, yk
 
 
@@ -727,6 +728,8 @@ def attention_description(n_q, n_kv, dh, Tq, Tk, start, length, k_start=None, k_
     k = (start, length) if single else (k_start, k_len)
     _dev(*q, *k, prefix, slopes)
     n_seq = length.numel()
+    if any(t is not None and t.device != length.device for t in (*q, *k, prefix, slopes)):
+        raise ValueError("attention_description: the tensors are on several devices")
     if any(t is not None and (t.dtype != torch.int32 or t.numel() != n_seq) for t in (*q, *k, prefix)):
         raise ValueError("attention_description: starts, lengths and prefixes are int32 [n_seq]")
     if slopes is not None and (slopes.dtype != torch.float32 or slopes.numel() != n_q):
@@ -747,8 +750,9 @@ def faar_attention_plan(a, out=None):
     """The plan of a description's masks, read by the calls of every layer -> uint8 device tensor."""
     _dev(out)
     n = int(lib().faar_attention_plan_bytes(ctypes.byref(a)))
-    plan = torch.empty(n, dtype=torch.uint8, device=a._device) if out is None else out
-    _check(lib().faar_attention_plan(ctypes.byref(a), _ptr(plan), plan.numel(), _stream()), "faar_attention_plan")
+    plan = torch.empty(max(n, 16), dtype=torch.uint8, device=a._device) if out is None else out
+    _check(lib().faar_attention_plan(ctypes.byref(a), _ptr(plan), plan.numel(), _raw_stream(plan, *a._keep)),
+           "faar_attention_plan")
     return plan
 
 
@@ -761,7 +765,8 @@ def attention_masked_workspace(a, backward=False):
 
 
 class AttentionStats:
-    """What a forward call keeps for its backward: lse float32 [n_q, Tq] and the low bytes of o, int8 [Tq, n_q * dh]."""
+    """What a forward call keeps for its backward: lse float32 [n_q, Tq] and the low bytes of o, int8 [Tq, n_q * dh].  Rows of no sequence
+    hold nothing."""
     __slots__ = ("lse", "o_low")
 
     def __init__(self, lse, o_low):
@@ -796,7 +801,7 @@ def faar_attention_masked_fwd(a, plan, q, k, v, out=None, want_lse=True, ws=None
     d = _masked_call(a, where, plan, q, k, v, o, stats, ws)
     _check(lib().faar_attention_masked_fwd(d, plan.data_ptr(), plan.numel(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
                                            _at(stats.lse) if stats else None, _at(stats.o_low) if stats else None, ws.data_ptr(), ws.numel(),
-                                           _raw_stream(q)), where)
+                                           _raw_stream(q, k, v, o, plan, ws, a._keep[-1])), where)
     return o, stats
 
 
@@ -813,7 +818,8 @@ def faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, out=None, ws=None
             raise ValueError(f"{where}: a gradient has another row stride than what it belongs to")
     _check(lib().faar_attention_masked_bwd(d, plan.data_ptr(), plan.numel(), d_o.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                            o.data_ptr(), stats.lse.data_ptr(), _at(stats.o_low), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                           ws.data_ptr(), ws.numel(), _raw_stream(q)), where)
+                                           ws.data_ptr(), ws.numel(),
+                                           _raw_stream(q, k, v, o, d_o, dq, dk, dv, stats.lse, stats.o_low, plan, ws, a._keep[-1])), where)
     return dq, dk, dv
 
 

@@ -11,7 +11,7 @@
 //
 // Plan.  Sequence lengths live on the device.  A plan, made by one small launch for a batch and read by every layer, lists the work
 // items: tiles of 128 queries (forward, dq) and of 64 keys (dk, dv) that each lie inside one sequence, the most expensive first, or
-// for single tokens the pieces of the caches.  A workgroup reads its item with one scalar load; the grid is the largest number of
+// for single tokens the pieces of the caches.  A workgroup reads its item with one load; the grid is the largest number of
 // items that any lengths can give, and workgroups behind the last item end at once.
 //
 // Tiles, copies and products are those of the causal kernels (faar_attention.hip): 64-token tiles in LDS by asynchronous copies, two
@@ -162,7 +162,8 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
 
   if (single) {
     // pieces of whole blocks, as equal as the total over the sequences allows; every sequence has one at least
-    const int per = z.target == 0 ? 1 << 20 : static_cast<int>(max(1ull, (sums[0] + z.target - 1) / z.target));
+    // (no sequence has more than 2^23 blocks, whatever many that share a cache add up to)
+    const int per = z.target == 0 ? 1 << 23 : static_cast<int>(min(max(1ull, (sums[0] + z.target - 1) / z.target), 1ull << 23));
     for (int b0 = 0; b0 < n_seq; b0 += kPlanThreads) {
       const int b = b0 + tid;
       const int blocks = b < n_seq ? blocks_of(b) : 0, n = b < n_seq ? max(1, (blocks + per - 1) / per) : 0;
@@ -180,7 +181,7 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
         plan[z.seq_at + 2 * b] = first;
         plan[z.seq_at + 2 * b + 1] = n;
         for (int i = 0; i < n; ++i) {
-          const int j0 = min(kl, lo + i * per * kPieceKeys), j1 = min(kl, j0 + per * kPieceKeys);
+          const int j0 = lo + i * per * kPieceKeys, j1 = i + 1 < n ? j0 + per * kPieceKeys : kl;
           int* w = plan + z.q_at + kItemWords * (first + i);
           w[0] = b;
           w[1] = k_start[b] + j0;
@@ -265,7 +266,7 @@ k_attention_plan(const int* __restrict__ q_start, const int* __restrict__ q_len,
       const int extra = tid == 0 ? z.extra_q : z.extra_k;
       if (pass < 0) {
         const unsigned long long share = extra > 0 ? (total[tid] + extra - 1) / extra : 0x7FFFFFFFull;
-        most_of_piece[tid] = static_cast<int>(min(max(share, static_cast<unsigned long long>(kLeastPiece)), 0x3FFFFFFFull));
+        most_of_piece[tid] = static_cast<int>(min(max(share, static_cast<unsigned long long>(kLeastPiece)), 1ull << 30));
         per_cost[tid] = static_cast<float>(kBuckets) / static_cast<float>(min(longest[tid], most_of_piece[tid]) + 1);
       } else if (pass == 0) {                          // counts -> first place of each cost
         int at = 0;
@@ -325,6 +326,8 @@ struct Scores {
 __device__ __forceinline__ Scores scores_of(const MaskedDims& d, int head, bool biased) {
   return {d.c, d.cap_a, d.cap_b, d.ref, biased && d.slopes ? d.slopes[head] * kLog2e : 0.0f};
 }
+// from a reference maximum (units of log 2) and the sum of 2^(score - it): -inf where there is no key; a NaN stays one
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : m * kLn2 + logf(l); }
 // 1 / (1 + 2^(b q.k)) = (1 - tanh) / 2
 __device__ __forceinline__ float cap_half(const Scores& sc, float x) {
   return __builtin_amdgcn_rcpf(1.0f + fast_exp2(x * sc.b));
@@ -572,7 +575,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
     }
     return;
   }
-  const float inv = lr > 0.0f ? 1.0f / lr : 0.0f;      // a query that sees no key: 0
+  const float inv = lr == 0.0f ? 0.0f : 1.0f / lr;     // a query that sees no key: 0; a NaN stays one
   char* stage = reinterpret_cast<char*>(lds) + wave * RowStage<DH>::BYTES;
   static_assert(4 * RowStage<DH>::BYTES <= sizeof(lds), "rows fit in the stages");
 #pragma unroll
@@ -585,7 +588,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
       RowStage<DH>::put(stage, lane, dt, j, x, o_low != nullptr);
     }
   const int64_t t = (int64_t)row0 + 32 * wave, width = (int64_t)d.n_q * d.dh;
-  if (lse && hi == 0 && n < mine) lse[(int64_t)head * d.Tq + t + n] = lt > 0.0f ? st.mc * kLn2 + logf(lt) : -INFINITY;
+  if (lse && hi == 0 && n < mine) lse[(int64_t)head * d.Tq + t + n] = lse_of(st.mc, lt);
   RowStage<DH>::flush(stage, lane, mine, d.dh, O + t * d.ldo + head * d.dh, d.ldo, o_low ? o_low + t * width + head * d.dh : nullptr, width);
 }
 
@@ -612,13 +615,13 @@ k_masked_join_fwd(const int* __restrict__ plan, PlanTag tag, PlanSizes z, Masked
       r += stats[p * step + 256] * f;
       x[0] += v.x * f; x[1] += v.y * f; x[2] += v.z * f; x[3] += v.w * f;
     }
-    const float inv = r > 0.0f ? 1.0f / r : 0.0f;
+    const float inv = r == 0.0f ? 0.0f : 1.0f / r;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] *= inv;
     const uint2 o = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
     *reinterpret_cast<uint2*>(O + (row0 + row) * d.ldo + head * d.dh + col) = o;
     if (o_low) *reinterpret_cast<uint32_t*>(o_low + (row0 + row) * width + head * d.dh + col) = low_bytes(x, o);
-    if (lse && col == 0) lse[(int64_t)head * d.Tq + row0 + row] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+    if (lse && col == 0) lse[(int64_t)head * d.Tq + row0 + row] = lse_of(m, l);
   }
 }
 
@@ -1104,7 +1107,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
       o[1] = l;
       o[2] = r;
     } else if (lse) {
-      lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+      lse[(int64_t)head * d.Tq + seq] = lse_of(m, l);
     }
   }
   for (int i = tid; i < heads * d.dh; i += 256) {
@@ -1118,7 +1121,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
     } else {
       float mh, lh, rh;
       joined(h, mh, lh, rh);
-      O[(int64_t)seq * d.ldo + hd * d.dh + c] = static_cast<bf16_t>(f32_to_bf16(rh > 0.0f ? x / rh : 0.0f));
+      O[(int64_t)seq * d.ldo + hd * d.dh + c] = static_cast<bf16_t>(f32_to_bf16(rh == 0.0f ? 0.0f : x / rh));
     }
   }
 }
@@ -1161,8 +1164,8 @@ k_masked_join(const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims
       x = fmaf(xi[i], g, x);
     }
   }
-  if (on) O[(int64_t)seq * d.ldo + head * d.dh + threadIdx.x] = static_cast<bf16_t>(f32_to_bf16(r > 0.0f ? x / r : 0.0f));
-  if (lse && threadIdx.x == 0) lse[(int64_t)head * d.Tq + seq] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+  if (on) O[(int64_t)seq * d.ldo + head * d.dh + threadIdx.x] = static_cast<bf16_t>(f32_to_bf16(r == 0.0f ? 0.0f : x / r));
+  if (lse && threadIdx.x == 0) lse[(int64_t)head * d.Tq + seq] = lse_of(m, l);
 }
 
 }  // namespace

@@ -183,6 +183,10 @@ CASES = {
     "pairs_of_heads": Case(packed([130, 64, 200, 129, 65] * 3), 64, 32, 32, cap=5.0),
     "quads_of_heads": Case(packed([130, 64, 200, 129, 65] * 3), 64, 16, 24, window=100),
     "long": Case(packed([1500, 37]), 1, 1, 64, cap=30.0),
+    # every sequence at the start of a place of 160 rows, and queries and keys in places of different sizes
+    "padded": Case([(160 * b, n, 160 * b, n, 0) for b, n in enumerate([160, 1, 0, 97, 128])], 4, 2, 64, Tq=800, cap=50.0),
+    "padded_apart": Case([(64 * b, n, 200 * b, m, 5) for b, (n, m) in enumerate([(64, 200), (1, 3), (10, 64), (0, 9)])], 2, 1, 96, same=False, Tq=256,
+                         Tk=800),
 }
 
 
@@ -473,6 +477,20 @@ def test_wrong_plans_and_lengths_are_answered_with_nan():
 
 
 @pytest.mark.gpu
+def test_plan_of_very_many_tokens_over_one_cache():
+    """A million tokens that see one cache of 2^30 rows: 2^43 blocks of keys in all, one piece each."""
+    n, rows = 1 << 20, 1 << 30
+    length = torch.full((n,), rows, dtype=torch.int32, device="cuda")
+    length[5:7] = 0
+    a = faar.attention_description(1, 1, 8, n, rows, torch.zeros_like(length), length, single=True)
+    w = faar.faar_attention_plan(a).view(torch.int32)
+    assert int(w[8]) == 0 and int(w[10]) == n
+    items = w[16:16 + 16 * n].view(n, 16)
+    assert torch.equal(items[:, 0], torch.arange(n, dtype=torch.int32, device="cuda")) and torch.equal(items[:, 2], length)
+    assert not bool(items[:, 1].any()) and torch.equal(items[:, 3], length - 1) and bool((items[:, 4] == 1).all())
+
+
+@pytest.mark.gpu
 def test_rows_beyond_32_bit_offsets():
     """Keys and values whose rows lie 2^23 elements apart: the last ones are 5 billion elements in."""
     n, ld, dh = 600, 1 << 23, 64
@@ -488,6 +506,94 @@ def test_rows_beyond_32_bit_offsets():
     inside(host(faar.faar_attention_masked_fwd(a, faar.faar_attention_plan(a), dev(q), kd, vd)[0]), o_w, tol["o"], "single")
     a = faar.attention_description(1, 1, dh, 1, n, ints([0]), ints([1]), ints([0]), ints(lens))
     inside(host(faar.faar_attention_masked_fwd(a, faar.faar_attention_plan(a), dev(q), kd, vd)[0]), o_w, tol["o"], "tiles")
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    """One plan, a workspace a stream: calls in flight together give what each gives alone."""
+    c = CASES["one_head_long"]                             # tiles in pieces, which meet in the workspace
+    a, (q, k, v, d_o) = c.device()
+    plan = faar.faar_attention_plan(a)
+    def run(q, ws):
+        o, stats = faar.faar_attention_masked_fwd(a, plan, q, k, v, ws=ws)
+        return (o, stats.lse, *faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, ws=ws))
+    inputs = [q, (-q).contiguous()]
+    spaces = [faar.attention_masked_workspace(a, backward=True) for _ in inputs]
+    want = [run(x, w) for x, w in zip(inputs, spaces)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in inputs], [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = run(inputs[i], spaces[i])
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert all(torch.equal(t, u) for t, u in zip(x, y))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (10.0, False), (100.0, False), (0.0, True)])
+@pytest.mark.parametrize("n_q,n", [(1, 1300), (4, 150)])
+def test_a_nan_that_is_seen_stays_one(n_q, n, cap, slopes):
+    c = Case(packed([n, 70]), n_q, 1, 64, cap=cap, slopes=slopes)
+    a, (q, k, v, d_o) = c.device()
+    plan = faar.faar_attention_plan(a)
+    row, head = n - 20, n_q - 1
+    q[row, head * 64 + 5] = float("nan")
+    o, stats = faar.faar_attention_masked_fwd(a, plan, q, k, v)
+    dq, _, _ = faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats)
+    for t in (o, dq):
+        bad = torch.isnan(t).view(-1, n_q, 64)
+        assert bool(bad[row, head].all()) and int(bad.sum()) == 64
+    assert bool(torch.isnan(stats.lse[head, row])) and int(torch.isnan(stats.lse).sum()) == 1
+    # single tokens: in the first of two caches the key before the last
+    t = faar.attention_description(n_q, 1, 64, 2, c.Tk, ints([0, n]), ints([n, 70]), single=True, cap=cap, slopes=None if not slopes else a._keep[-1])
+    k[n - 2, 9] = float("nan")
+    o, stats = faar.faar_attention_masked_fwd(t, faar.faar_attention_plan(t), q[:2].contiguous(), k, v)
+    assert bool(torch.isnan(o[0]).all()) and not bool(torch.isnan(o[1]).any())
+    assert bool(torch.isnan(stats.lse[:, 0]).all()) and not bool(torch.isnan(stats.lse[:, 1]).any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[700, 1, 3000], [100, 7, 0]])
+def test_single_tokens_in_a_graph(lens):
+    """Tokens generated one after the other by replays of one graph: the lengths grow by one, the plan follows."""
+    n, cap_rows, n_q, n_kv, dh = len(lens), max(lens) + 8, 4, 2, 64
+    rng = np.random.default_rng(11)
+    q, k, v = (dev(rng.standard_normal((T, h * dh))) for T, h in ((n, n_q), (n * cap_rows, n_kv), (n * cap_rows, n_kv)))
+    length = ints(lens)
+    a = faar.attention_description(n_q, n_kv, dh, n, n * cap_rows, ints(b * cap_rows for b in range(n)), length, single=True, cap=30.0)
+    plan, ws = faar.faar_attention_plan(a), faar.attention_masked_workspace(a)
+    o = torch.empty_like(q)
+    def token():
+        faar.faar_attention_plan(a, out=plan)
+        return faar.faar_attention_masked_fwd(a, plan, q, k, v, out=o, want_lse=False, ws=ws)[0]
+    token()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        length.add_(1)
+        token()
+    for step in range(4):
+        o.fill_(float("nan"))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.clone()
+        assert length.tolist() == [x + step + 1 for x in lens]
+        assert torch.equal(got, token()) and not bool(torch.isnan(got).any())
+
+
+def test_tensors_of_other_devices_are_refused(monkeypatch):
+    class On:
+        def __init__(self, device):
+            self.get_device = lambda: device
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 77, raising=False)
+    assert fb._raw_stream(On(1), None, On(1)) == 77
+    for ts in ((On(0),), (On(1), On(0)), (On(1), None, On(-1))):
+        with pytest.raises(ValueError, match="another device"):
+            fb._raw_stream(*ts)
 
 
 def test_refusals():

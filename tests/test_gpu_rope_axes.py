@@ -95,6 +95,29 @@ def test_equal_positions_on_every_axis_are_the_one_axis_embedding():
     assert np.all(np.abs(host(got) - w) <= 2 * U8 * np.abs(w) + 2e-6 * size)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 2050])
+def test_streams_and_graphs_of_positions_that_change(T):
+    H, dh = 3, 64
+    rng, pos, axis, freq = setup(T, 2, dh // 2, 4096, 4)
+    q, pd = dev(rng.standard_normal((T, H * dh))), torch.from_numpy(pos).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got, _ = faar.faar_rope_axes(q, None, H, 0, dh, pd, axis, freq)
+    side.synchronize()
+    assert torch.equal(got, faar.faar_rope_axes(q, None, H, 0, dh, pd, axis, freq)[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held, _ = faar.faar_rope_axes(q, None, H, 0, dh, pd, axis, freq)
+    for step in range(3):
+        pd.add_(1)
+        held.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, faar.faar_rope_axes(q, None, H, 0, dh, pd, axis, freq)[0])
+
+
 def test_refusals():
     L = fb.lib()
     p, odd, nul = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1004), None
