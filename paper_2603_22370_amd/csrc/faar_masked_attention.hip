@@ -1176,7 +1176,8 @@ PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_
   if (single) {
     const int64_t cols = n_kv * ((n_q / n_kv + 31) / 32);
     // pieces: about 512 workgroups; small caches in one piece each, since joining costs as much as walking four blocks of
-    // keys (700 keys, 8 heads of 64, on the device: six pieces and their join 5.5 + 3.2 us, whole 10.3)
+    // keys.  Pieces with their join against whole, on the device: 512 rows, 16 heads of 128 7.0 + 2.8 against 9.2 us and 8 heads of 64
+    // 5.8 + 2.9 against 6.8; but 700 rows, 8 heads of 64 5.5 + 3.2 against 10.3
     z.target = Tk <= kSmallCaches ? 0 : static_cast<int>((512 + cols - 1) / cols);
     z.max_q = n_seq + z.target;
     z.seq_at = static_cast<int>(z.q_at + kItemWords * z.max_q);

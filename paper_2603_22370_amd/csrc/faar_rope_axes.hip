@@ -6,7 +6,8 @@
 // its fraction, at most half a turn, goes on in float32.
 //
 // HBM-bound (2 bytes in, 2 out an element), provided that the 64-bit products, the sine and the cosine are not taken per element:
-// a workgroup makes those of its tokens once, into LDS, and applies them to all heads of q and k.
+// a workgroup makes those of its tokens once, into LDS, and applies them to all heads of q and k.  201 MB (16384 tokens, 16 + 8
+// heads of 128) in 40 us, the rate of a large copy; 24 tokens take 2.6 us on the device.
 #include "faar_internal.h"
 
 namespace faar {
@@ -79,7 +80,9 @@ k_rope_axes(RopeTensor q, RopeTensor k, int64_t T, int dh, int half, const int32
 hipError_t launch_rope_axes(const RopeTensor& q, const RopeTensor& k, int64_t T, int dh, int half, const int32_t* pos, const RopeAxes& ax,
                             bool inverse, bool pairs, bool copy_rest, hipStream_t st) {
   const float sign = inverse ? -1.0f : 1.0f;
-  // four tokens a workgroup give each of its threads one sine at 64 frequencies; few tokens spread over the device one by one
+  // four tokens a workgroup give each of its threads one sine at 64 frequencies; few tokens spread over the device one by one.  One / four
+  // a workgroup, 16 + 8 heads of 128 and 8 + 8 of 64 taken together, in us: 64 tokens 3.6 / 4.5, 512 4.1 / 5.1, 2048 6.6 / 6.6,
+  // 8192 18.0 / 15.4, 40000 97 / 87
   if (T >= 2048)
     hipLaunchKernelGGL(k_rope_axes<4>, dim3(static_cast<unsigned>((T + 3) / 4)), dim3(kEltThreads), 0, st, q, k, T, dh, half, pos, ax, sign, pairs, copy_rest);
   else
