@@ -647,13 +647,13 @@ __device__ __forceinline__ float prob_of(float x, const Scores& sc, float shift,
 // ahead, as in the dk / dv kernel, and for its reason: with all of them requested at once registers run out.
 template <class H, bool kCap, bool kBias>
 __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x8 (&qf)[H::KS], const bf16x8 (&dof)[H::KS], float shift,
-                                               float dl, uint32_t k_rows, uint32_t v_rows, uint32_t k_cols, const Scores& sc, bool masked,
+                                               const f32x16& less, uint32_t k_rows, uint32_t v_rows, uint32_t k_cols, const Scores& sc, bool masked,
                                                int first, int len, float gap) {
   constexpr int DH = H::DH, KS = H::KS, DT = H::DT;
   typedef Tile<DH> Tl;
   constexpr int kRing = 4;
   bf16x8 f[kRing];
-  f32x16 s = zero16(), dp = zero16();      // rows = keys, column = query
+  f32x16 s = zero16(), dp = less;          // rows = keys, column = query; dP starts at -delta, which saves the subtraction
   auto fetch_rows = [&](int i) { f[i % kRing] = Tl::rows(i & 1 ? v_rows : k_rows, 0, i / 2); };
 #pragma unroll
   for (int i = 0; i < kRing - 1; ++i) fetch_rows(i);
@@ -669,7 +669,7 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
     const int j = 8 * (v / 4) + v % 4;
     float slack = 1.0f;
     float p = prob_of<kCap, kBias>(s[v], sc, shift, gap - static_cast<float>(j), slack);
-    dp[v] = p * (dp[v] - dl);
+    dp[v] *= p;
     if constexpr (kCap) dp[v] *= slack;
   }
   if (masked) {
@@ -718,9 +718,19 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
   const Seen sa = keys_of(pos0 + 32 * wave, k_len, prefix, window, causal), sb = keys_of(pos0 + 32 * wave + mine - 1, k_len, prefix, window, causal);
   const int64_t t0 = (int64_t)row0 + 32 * wave + n;
 
+  const int64_t kvcol = (int64_t)kvh * d.dh;
+  const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
+  const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
+  auto request = [&](int kb) {
+    const uint32_t at = lds0 + (kb & 1) * (2 * Tl::ELEMS * 2);
+    copy_tile<DH>(K, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
+    copy_tile<DH>(V, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldv, kvcol, d.dh, from_v, at + Tl::ELEMS * 2, wave, tid);
+  };
+  clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
+  if (kb0 < kb1) request(kb0);
   bf16x8 qf[KS], dof[KS];
   float shift = 0.0f, dl = 0.0f;
-  f32x16 acc[DT];
+  const float lse0 = live ? lse[(int64_t)head * d.Tq + t0] : 0.0f;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const bool on = live && ks * 16 + 8 * hi < d.dh;
@@ -737,24 +747,17 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
   }
   dl = half_sum(dl);
   if (live) {
-    shift = (kCap ? sc.a : 0.0f) - lse[(int64_t)head * d.Tq + t0] * kLog2e;
+    shift = (kCap ? sc.a : 0.0f) - lse0 * kLog2e;
     if (hi == 0) {
-      delta[(int64_t)head * d.Tq + t0] = dl;
+      delta[(int64_t)head * d.Tq + t0] = -dl;
       delta[((int64_t)d.n_q + head) * d.Tq + t0] = shift;
     }
   }
+  f32x16 acc[DT], less;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
-  const int64_t kvcol = (int64_t)kvh * d.dh;
-  const uint32_t lds0 = lds_addr_of(lds), ra = Tl::rows_at(lane), ca = Tl::cols_at(lane);
-  const uint32_t from_k = Tl::of_lane(d.ldk, tid), from_v = Tl::of_lane(d.ldv, tid);
-  auto request = [&](int kb) {
-    const uint32_t at = lds0 + (kb & 1) * (2 * Tl::ELEMS * 2);
-    copy_tile<DH>(K, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldk, kvcol, d.dh, from_k, at, wave, tid);
-    copy_tile<DH>(V, (int64_t)k_start + kb * kTok, k_len - kb * kTok, d.ldv, kvcol, d.dh, from_v, at + Tl::ELEMS * 2, wave, tid);
-  };
-  clear_columns<H>(&lds[0][0][0], 4, d.dh, tid);
-  if (kb0 < kb1) request(kb0);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) less[v] = -dl;
   for (int kb = kb0; kb < kb1; ++kb) {
     FAAR_WAIT_VMCNT(0);
     __syncthreads();
@@ -768,7 +771,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
 #pragma unroll 1
     for (int kt = 0; kt < 2; ++kt) {
       const uint32_t half = kt * (32 * DH * 2);
-      masked_dq_tile<H, kCap, kBias>(acc, qf, dof, shift, dl, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
+      masked_dq_tile<H, kCap, kBias>(acc, qf, dof, shift, less, k_lds + ra + half, v_lds + ra + half, k_lds + ca + half, sc, !whole, first + 32 * kt, len,
                                       gap - 32 * kt);
     }
   }
@@ -803,7 +806,12 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
   typedef Tile<DH> Tl;
   constexpr int kRing = 3;
   bf16x8 f[kRing];
-  f32x16 s = zero16(), dp = zero16();      // rows = queries, column = key
+  f32x16 s = zero16(), dp;                 // rows = queries, column = key; dP starts at -delta, which saves the subtraction
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float4 d4 = *reinterpret_cast<const float4*>(delta_lds + 8 * j + 4 * (lane >> 5));
+    dp[4 * j] = d4.x; dp[4 * j + 1] = d4.y; dp[4 * j + 2] = d4.z; dp[4 * j + 3] = d4.w;
+  }
   auto fetch_rows = [&](int i) { f[i % kRing] = Tl::rows(q_rows + (i & 1) * kDo, 0, i / 2); };
 #pragma unroll
   for (int i = 0; i < kRing - 1; ++i) fetch_rows(i);
@@ -818,14 +826,13 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
   for (int j = 0; j < 4; ++j) {
     const int row = 8 * j + 4 * (lane >> 5);
     const float4 l4 = *reinterpret_cast<const float4*>(shift_lds + row);
-    const float4 d4 = *reinterpret_cast<const float4*>(delta_lds + row);
-    const float lr[4] = {l4.x, l4.y, l4.z, l4.w}, dr[4] = {d4.x, d4.y, d4.z, d4.w};
+    const float lr[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float slack = 1.0f;
       float p = prob_of<kCap, kBias>(s[4 * j + r], sc, lr[r], gap + static_cast<float>(8 * j + r), slack);
       s[4 * j + r] = p;
-      float g = p * (dp[4 * j + r] - dr[r]);
+      float g = p * dp[4 * j + r];
       if constexpr (kCap) g *= slack;
       dp[4 * j + r] = g;
     }
