@@ -9,7 +9,8 @@
 // (b+1)*S-1, S a multiple of 32; query head j reads key / value head j / (n_q / n_kv).
 //
 // A workgroup of four wavefronts owns 128 query positions (forward, dq) or 128 key positions (dk, dv) of one head and
-// sequence, 32 per wavefront, and walks the causal range in blocks of 64 tokens whose tiles it shares through LDS (Tile).  Products run as v_mfma_f32_32x32x16_bf16:
+// sequence, 32 per wavefront, and walks the causal range in blocks of 64 tokens whose tiles it shares through LDS (Tile).  Products
+// run as v_mfma_f32_32x32x16_bf16:
 //   * a product whose contraction runs over dh takes rows of a tile as they lie there (16-byte LDS reads);
 //   * a product whose contraction runs over tokens (P V, dS K, P^T dO, dS^T Q) takes COLUMNS of the same tile through the LDS
 //     transposing reads of this architecture (ds_read_b64_tr_b16): no transposed copy exists anywhere;
