@@ -697,7 +697,7 @@ typedef struct {
   int64_t n_q, n_kv, dh;   /* n_q % n_kv == 0; dh a multiple of 8, at most 128 */
   int64_t ldq, ldk, ldv, ldo; /* elements between rows of q (and dq), k (dk), v (dv), o (d_o): multiples of 8, heads side by side in a
                                  row; q, k and v may be parts of one buffer, and so may their gradients */
-  float scale;             /* > 0 */
+  float scale;             /* > 0, at most 2^126 */
   float cap;               /* 0: none */
   const float* slopes;     /* in  device float[n_q], nullable: finite */
 } faar_attention;
@@ -713,13 +713,14 @@ int faar_attention_plan(const faar_attention* a, void* plan, size_t plan_bytes, 
 
 /* q in bf16 [Tq] rows of n_q * dh, k, v in bf16 [Tk] rows of n_kv * dh, o out bf16; kept for the backward: lse out, nullable float [n_q * Tq],
  * and o_low out, nullable int8 [Tq][n_q * dh]: what the rounding took from o, in 2^-8 of its last place (not with single tokens).
- * float32 arithmetic; probabilities are rounded to bf16 as matrix-core operands. */
+ * float32 arithmetic; probabilities are rounded to bf16 as matrix-core operands.  Outputs must not overlap inputs (FAAR_E_ARG where one
+ * starts where an input does). */
 int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* q, const void* k, const void* v, void* o,
                               float* lse, uint8_t* o_low, void* ws, size_t ws_bytes, void* stream);
 
 /* (dq, dk, dv) for the output gradient d_o; o, lse and o_low from the forward call.  o_low may be NULL: the gradients of queries whose
  * softmax is sharp then carry the rounding of o, many times over.  dk and dv are summed over the query heads of a group in a fixed
- * order.  Outputs must not overlap inputs. */
+ * order.  Outputs must not overlap inputs (FAAR_E_ARG where one starts where an input does). */
 int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* d_o, const void* q, const void* k,
                               const void* v, const void* o, const float* lse, const uint8_t* o_low, void* dq, void* dk, void* dv, void* ws,
                               size_t ws_bytes, void* stream);

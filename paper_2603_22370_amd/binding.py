@@ -262,6 +262,14 @@ def _zeros_like_rows(t):
     return t.new_zeros((t.shape[0], max(t.stride(0), t.shape[1])))[:, :t.shape[1]]
 
 
+def _gradients_of(q, k, v):
+    """Zeros with the shapes and row strides of q, k and v: where those have the rows of one buffer, parts of one buffer, in that order."""
+    widths = [t.shape[1] for t in (q, k, v)]
+    if q.shape[0] == k.shape[0] and q.stride(0) == k.stride(0) == v.stride(0) and sum(widths) <= q.stride(0):
+        return q.new_zeros((q.shape[0], q.stride(0)))[:, :sum(widths)].split(widths, dim=1)
+    return tuple(_zeros_like_rows(t) for t in (q, k, v))
+
+
 def _check(rc: int, where: str):
     if rc != 0:
         raise FaarError(rc, where)
@@ -806,10 +814,10 @@ def faar_attention_masked_fwd(a, plan, q, k, v, out=None, want_lse=True, ws=None
 
 
 def faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, out=None, ws=None):
-    """-> (dq, dk, dv) bf16, shaped like q, k, v (out: the same three, with the row strides of q, k and v).  Rows of no sequence keep what
-    out holds (0 where out is not given)."""
+    """-> (dq, dk, dv) bf16, shaped like q, k, v (out: the same three, with the row strides of q, k and v; not given, parts of one
+    buffer where q, k and v are).  Rows of no sequence keep what out holds (0 where out is not given)."""
     where = "faar_attention_masked_bwd"
-    dq, dk, dv = tuple(_zeros_like_rows(t) for t in (q, k, v)) if out is None else out
+    dq, dk, dv = _gradients_of(q, k, v) if out is None else out
     if ws is None:
         ws = attention_masked_workspace(a, backward=True)
     d = _masked_call(a, where, plan, q, k, v, o, stats, ws)

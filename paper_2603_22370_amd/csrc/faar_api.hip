@@ -1023,7 +1023,7 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
   for (int i = 0; i < kPlanTagWords; ++i) c.tag.w[i] = tag[i];
   constexpr float kL2e = 1.4426950408889634f;
   const float cap_a = a->cap * kL2e, cap_b = a->cap > 0.0f ? 2.0f * kL2e * a->scale / a->cap : 0.0f;
-  if (!std::isfinite(cap_a) || !std::isfinite(cap_b) || !std::isfinite(a->scale * 4.0f)) return FAAR_E_ARG;
+  if (!std::isfinite(cap_a) || !std::isfinite(cap_b) || a->scale > 0x1p126f) return FAAR_E_ARG;
   c.d = MaskedDims{static_cast<int>(a->n_q), static_cast<int>(a->n_kv), static_cast<int>(a->dh), a->Tq, a->Tk, a->ldq, a->ldk, a->ldv, a->ldo,
                    a->cap > 0.0f ? 4.0f * a->scale : a->scale, a->scale * kL2e, cap_a, cap_b, std::min(cap_a, 110.0f - cap_a), a->slopes};
   return FAAR_OK;
@@ -1076,6 +1076,7 @@ int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t 
       (reinterpret_cast<uintptr_t>(lse) & 3u))
     return FAAR_E_ARG;
   if (plan_bytes < align256((size_t)c.z.words * 4) || !ws || ws_bytes < masked_ws_bytes(c, false)) return FAAR_E_WORKSPACE;
+  if (o == q || o == k || o == v) return FAAR_E_ARG;
   return hip_status(launch_masked_fwd(static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v),
                                       static_cast<const int*>(plan), c.tag, c.z, c.d, c.single, static_cast<bf16_t*>(o), lse, o_low,
                                       static_cast<float*>(ws), static_cast<hipStream_t>(stream)));
@@ -1093,6 +1094,9 @@ int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t 
     if (!aligned16(p)) return FAAR_E_ARG;
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return FAAR_E_ARG;
   if (plan_bytes < align256((size_t)c.z.words * 4) || !ws || ws_bytes < masked_ws_bytes(c, true)) return FAAR_E_WORKSPACE;
+  for (const void* out : {dq, dk, dv})
+    for (const void* in : {d_o, q, k, v, o})
+      if (out == in) return FAAR_E_ARG;
   return hip_status(launch_masked_bwd(static_cast<const bf16_t*>(d_o), static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k),
                                       static_cast<const bf16_t*>(v), static_cast<const bf16_t*>(o), o_low, lse, static_cast<const int*>(plan), c.tag,
                                       c.z, c.d, static_cast<float*>(ws), static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk), static_cast<bf16_t*>(dv),

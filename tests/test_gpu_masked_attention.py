@@ -509,6 +509,22 @@ def test_rows_beyond_32_bit_offsets():
 
 
 @pytest.mark.gpu
+def test_gradients_that_are_not_given_places():
+    """Of q, k and v in one buffer they come in one buffer, else each in its own; rows of no sequence are 0."""
+    for name in ("prefix_cap_bias_fused", "mixed_causal"):
+        c = CASES[name]
+        a, (q, k, v, d_o) = c.device()
+        plan = faar.faar_attention_plan(a)
+        o, stats = faar.faar_attention_masked_fwd(a, plan, q, k, v)
+        given = faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats, out=[fb._zeros_like_rows(t) for t in (q, k, v)])
+        got = faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats)
+        assert all(torch.equal(x, y) for x, y in zip(got, given))
+        assert not host(got[0])[~c.q_rows].any() and not host(got[2])[~c.k_rows].any()
+        one = len({x.untyped_storage().data_ptr() for x in got}) == 1
+        assert one == c.fused and [x.stride(0) for x in got] == [x.stride(0) for x in (q, k, v)]
+
+
+@pytest.mark.gpu
 def test_two_streams_at_once():
     """One plan, a workspace a stream: calls in flight together give what each gives alone."""
     c = CASES["one_head_long"]                             # tiles in pieces, which meet in the workspace
@@ -647,3 +663,22 @@ def test_refusals():
     r = ctypes.byref(t)
     assert L.faar_attention_plan_bytes(r) > 0 and L.faar_attention_masked_workspace_bytes(r, 0) > 4 * 66 * 4
     assert L.faar_attention_masked_workspace_bytes(r, 1) == 0 and bwd(r) == -7 and fwd(r, low=P) == -7
+
+
+def test_outputs_in_the_place_of_inputs_are_refused():
+    L, nul, big = fb.lib(), None, 1 << 40
+    a = fb.faar_attention()
+    a.n_seq, a.Tq, a.Tk, a.q_start, a.q_len, a.n_q, a.n_kv, a.dh, a.scale = 1, 64, 64, 0x1000, 0x1000, 2, 2, 64, 0.125
+    a.ldq = a.ldo = a.ldk = a.ldv = 128
+    r, at = ctypes.byref(a), [ctypes.c_void_p(0x100000 * (i + 1)) for i in range(10)]
+    plan, ws, lse, d_o, q, k, v, o, dq, dk = at
+    dv = ctypes.c_void_p(0x2000000)
+    for out in (q, k, v):
+        assert L.faar_attention_masked_fwd(r, plan, big, q, k, v, out, lse, nul, ws, big, nul) == -6
+    for place in (d_o, q, k, v, o):
+        for i in range(3):
+            outs = [dq, dk, dv]
+            outs[i] = place
+            assert L.faar_attention_masked_bwd(r, plan, big, d_o, q, k, v, o, lse, nul, *outs, ws, big, nul) == -6
+    a.scale = 2.0 ** 127
+    assert L.faar_attention_plan(r, plan, big, nul) == -6
