@@ -3,9 +3,9 @@ only.  torch is used for device memory and streams; every step of the method run
 kernels behind the C ABI.  There is no fallback: a missing library raises."""
 from __future__ import annotations
 
-import array
 import ctypes
 import os
+import struct
 from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 import torch
@@ -625,7 +625,9 @@ def faar_layernorm_fwd(x, g, b=None, eps=1e-5):
     _whole(g, _F32, D, where)
     if b is not None:
         _whole(b, _F32, D, where)
-    h, mean, rstd = x.new_empty((T, D), dtype=_BF16), x.new_empty(T, dtype=_F32), x.new_empty(T, dtype=_F32)
+    h = torch.empty_like(x) if x.dtype is _BF16 else x.new_empty((T, D), dtype=_BF16)
+    mean = x.new_empty(T, dtype=_F32)
+    rstd = torch.empty_like(mean)
     _check(lib().faar_layernorm_fwd(x.data_ptr(), _dt(x), T, D, g.data_ptr(), _at(b), eps, h.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
                                     _raw_stream(x, g, b)), where)
     return h, mean, rstd
@@ -674,16 +676,15 @@ def faar_rope_axes(q, k, n_q, n_k, dh, pos, axis, freq, pairs=False, inverse=Fal
     ldq = _row_stride(q, T, n_q * dh, where)
     ldk = 0 if k is None else _row_stride(k, T, n_k * dh, where)
     if out is None:
-        yq, yk = q.new_empty((T, n_q * dh)), None if k is None else k.new_empty((T, n_k * dh))
+        yq, yk = torch.empty_like(q), None if k is None else torch.empty_like(k)      # rows side by side, wherever q's and k's lie
         ldyq, ldyk = n_q * dh, n_k * dh
     else:
         yq, yk = out
         if (k is None) != (yk is None):
             raise ValueError("faar_rope_axes: k and its output come together")
         ldyq, ldyk = _row_stride(yq, T, n_q * dh, where), 0 if k is None else _row_stride(yk, T, n_k * dh, where)
-    fr = array.array("d", freq)
     _check(lib().faar_rope_axes(q.data_ptr(), ldq, n_q, _at(k), ldk, n_k, T, dh, 2 * half, pos.data_ptr(), n_axes, bytes(list(axis)),
-                                fr.buffer_info()[0], (FAAR_ROPE_PAIRS if pairs else 0) | (FAAR_ROPE_INVERSE if inverse else 0), yq.data_ptr(),
+                                struct.pack(f"{half}d", *freq), (FAAR_ROPE_PAIRS if pairs else 0) | (FAAR_ROPE_INVERSE if inverse else 0), yq.data_ptr(),
                                 ldyq, _at(yk), ldyk, _raw_stream(q, k, pos, yq, yk)), where)
     return yq, yk
 
