@@ -82,10 +82,12 @@ __device__ __forceinline__ uint32_t lds_addr_of(const void* p) {
 #define FAAR_WAIT_VMCNT(N) __builtin_amdgcn_s_waitcnt(0x0F70 | ((N)&0xF) | (((N) >> 4) << 14))
 
 // A [64 tokens][dh] tile of a token-major tensor in LDS, rows un-padded.  The 16-byte chunks of a row are stored XOR-permuted
-// by a key of the row so that both kinds of read spread over the 64 banks: the 16 rows of a 16-byte row read fall on 16
-// distinct chunk positions, and the 16 32-byte segments of a transposing read (8 tokens x 2 groups of 16 columns) on the 8 bank
-// groups twice each.  dh = 128: a row is one turn of the banks, key = row bits 0..2 on chunk bits 1..3 (which 32-byte pair)
-// and row bit 3 on chunk bit 0; dh = 64: two rows to a turn, key = row bits 1, 2 on chunk bits 1, 2 and row bit 3 on bit 0.
+// by a key of the row so that both kinds of read spread over the 64 banks, which serve 16 lanes of a 16-byte row read or 32 of an
+// 8-byte transposing read at a time: the 16 rows of the one fall on 16 distinct chunk positions, and the 8 32-byte segments of the
+// other (4 tokens x 2 groups of 16 columns) on the 8 bank groups once each.  dh = 128: a row is one turn of the banks, and its bits
+// 0, 1, 2, 3 go to bits 2, 3, 1, 0 of the chunk (bits 1..3: which 32-byte segment, bit 1 the group of 16 columns); dh = 64: two rows
+// to a turn, bits 1, 2, 3 to bits 2, 1, 0.  (With row bits in order, which keeps 64 lanes apart but not each 32, every transposing
+// read took twice the cycles.)
 template <int DH>
 struct Tile {
   static constexpr int CPR = DH / 8;                  // 16-byte chunks per row
@@ -93,7 +95,7 @@ struct Tile {
   static constexpr int ELEMS = kTok * DH;
 
   static __device__ __forceinline__ int key(int row) {
-    return (DH == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3)) | ((row >> 3) & 1);
+    return (DH == 128 ? 4 * (row & 3) : 2 * (row & 2)) | ((row >> 1) & 2) | ((row >> 3) & 1);
   }
   // rows row0 .. row0+63, columns col0 .. col0+dh-1, global -> LDS without passing through registers: chunk i = tid + 256 j of
   // the tile lands at byte 16 i.  A pass of the workgroup covers 2048 / dh rows, a divisor of 32, and starts at a row whose key
