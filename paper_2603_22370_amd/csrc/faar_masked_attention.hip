@@ -48,8 +48,8 @@ __device__ __forceinline__ void dma16_from(const void* gptr, uint32_t lds_addr) 
 struct Heads64 { static constexpr int DH = 64, KS = 4, DT = 2; };
 struct Heads96 { static constexpr int DH = 128, KS = 6, DT = 3; };    // a row as of 128, of which the last quarter is never touched
 struct Heads128 { static constexpr int DH = 128, KS = 8, DT = 4; };
-// Products over dh leave out the last step where no head reaches it (13 images of 10007 patches, heads of 80: forward 121.6 -> 120.3 us, dq 150.9 -> 146.3, dk and dv 222.3 -> 219.4;
-// not with 128, whose dk and dv have no register left for it)
+// Products over dh leave out the last step where no head reaches it (13 images of 10007 patches, heads of 80: forward 121.6 -> 120.3 us,
+// dq 150.9 -> 146.3, dk and dv 222.3 -> 219.4; not with 128, whose dk and dv have no register left for it)
 template <class H> __device__ __forceinline__ bool uses_last(int dh) { return H::KS == 8 || dh > 16 * (H::KS - 1); }
 
 // 64 rows of a tile of which `valid` are there, dh columns of each.  Columns beyond dh are left alone (clear_columns); rows that are
@@ -979,25 +979,33 @@ k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, con
                                      static_cast<float>(at + off - key), lane);
   }
   // the two wavefronts of a block of keys: one hands over its dv and finishes dk, the other the reverse
-  f32x16* give = reinterpret_cast<f32x16*>(lds) + (size_t)wave * DT * 64 + lane;
-  const f32x16* take = reinterpret_cast<const f32x16*>(lds) + (size_t)(wave ^ 2) * DT * 64 + lane;
-  static_assert(4 * DT * 64 * sizeof(f32x16) <= sizeof(lds), "exchange fits in the stages");
+  // (four values a lane at a time, side by side: no bank conflicts)
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4* give = reinterpret_cast<f32x4*>(lds) + (size_t)wave * DT * 256 + lane;
+  const f32x4* take = reinterpret_cast<const f32x4*>(lds) + (size_t)(wave ^ 2) * DT * 256 + lane;
+  static_assert(4 * DT * 256 * sizeof(f32x4) <= sizeof(lds), "exchange fits in the stages");
   __syncthreads();
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
-    f32x16 g;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) g[i] = qw == 0 ? dv[dt][i] : dk[dt][i];
-    give[dt * 64] = g;
+    for (int j = 0; j < 4; ++j) {
+      f32x4 g;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = qw == 0 ? dv[dt][4 * j + i] : dk[dt][4 * j + i];
+      give[(dt * 4 + j) * 64] = g;
+    }
   }
   __syncthreads();
   f32x16 sum[DT];
   const float k = qw == 0 && slot < 0 ? d.grad_scale : 1.0f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
-    const f32x16 r = take[dt * 64];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum[dt][i] = ((qw == 0 ? dk[dt][i] : dv[dt][i]) + r[i]) * k;
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 r = take[(dt * 4 + j) * 64];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[dt][4 * j + i] = ((qw == 0 ? dk[dt][4 * j + i] : dv[dt][4 * j + i]) + r[i]) * k;
+    }
   }
   if (slot >= 0) {                                     // a piece: [dk, dv][64 rows][dh] sums
     leave_sums<H>(sum, part + ((((int64_t)slot * d.n_kv + kvh) * 2 + qw) * 64 + 32 * kw) * d.dh, mine, d.dh, again(lane));
