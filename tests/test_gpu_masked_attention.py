@@ -525,6 +525,21 @@ def test_gradients_that_are_not_given_places():
 
 
 @pytest.mark.gpu
+def test_one_plan_for_layers_that_differ():
+    """A plan depends on the sequences, the mask and the heads alone: layers with other widths, caps and biases read the same one."""
+    seqs, plan = packed([33, 140, 90], prefix=50, gap=3), None
+    for dh, cap, slopes in ((64, 20.0, True), (104, 0.0, False), (24, 100.0, False)):
+        c = Case(seqs, 6, 2, dh, cap=cap, slopes=slopes)
+        (o_w, _, dq_w, dk_w, dv_w), tol = c.oracle()
+        a, (q, k, v, d_o) = c.device()
+        plan = faar.faar_attention_plan(a) if plan is None else plan
+        o, stats = faar.faar_attention_masked_fwd(a, plan, q, k, v)
+        inside(host(o)[c.q_rows], o_w[c.q_rows], tol["o"][c.q_rows], "o")
+        for g, w, n in zip(faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats), (dq_w, dk_w, dv_w), ("dq", "dk", "dv")):
+            inside(host(g)[c.q_rows], w[c.q_rows], tol[n][c.q_rows], n)
+
+
+@pytest.mark.gpu
 def test_two_streams_at_once():
     """One plan, a workspace a stream: calls in flight together give what each gives alone."""
     c = CASES["one_head_long"]                             # tiles in pieces, which meet in the workspace
