@@ -1025,7 +1025,8 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
   const float cap_a = a->cap * kL2e, cap_b = a->cap > 0.0f ? 2.0f * kL2e * a->scale / a->cap : 0.0f;
   if (!std::isfinite(cap_a) || !std::isfinite(cap_b) || a->scale > 0x1p126f) return FAAR_E_ARG;
   c.d = MaskedDims{static_cast<int>(a->n_q), static_cast<int>(a->n_kv), static_cast<int>(a->dh), a->Tq, a->Tk, a->ldq, a->ldk, a->ldv, a->ldo,
-                   a->cap > 0.0f ? 4.0f * a->scale : a->scale, a->scale * kL2e, cap_a, cap_b, std::min(cap_a, 110.0f - cap_a), a->slopes};
+                   a->cap > 0.0f ? 4.0f * a->scale : a->scale, a->scale * kL2e, cap_a, cap_b,
+                   a->cap > 0.0f ? a->scale / a->cap : 0.0f, std::min(cap_a, 110.0f - cap_a), a->slopes};
   return FAAR_OK;
 }
 

@@ -199,7 +199,7 @@ struct PlanSizes { int q_at, k_at, seq_at, join_at[2], target, extra_q, extra_k;
 struct MaskedDims {
   int n_q, n_kv, dh;
   int64_t Tq, Tk, ldq, ldk, ldv, ldo;   // rows; elements between rows
-  float grad_scale, c, cap_a, cap_b, ref;    // of dq and dk: scale, capped 4 scale; c = scale log2 e; cap_a = cap log2 e (0: none), cap_b = 2 scale log2 e / cap; ref: see launch_masked_fwd
+  float grad_scale, c, cap_a, cap_b, cap_t, ref;   // of dq and dk: scale, capped 4 scale; c = scale log2 e; cap_a = cap log2 e (0: none), cap_b = 2 scale log2 e / cap, cap_t = scale / cap; ref: see launch_masked_fwd
   const float* slopes;                  // nullable [n_q]
 };
 PlanSizes attention_plan_sizes(int64_t n_seq, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, bool single);

@@ -35,8 +35,10 @@ constexpr float kLowest = -1.7e38f;    // "no score yet": below every score, and
 constexpr float kLazy = 8.0f;          // the reference maximum is raised when a score exceeds it by more than 2^kLazy
 
 // how scores become exponents: as they are; with a bias; capped with every exponent in range of a fixed reference; capped with a
-// running maximum (and a bias)
-enum { kPlain = 0, kBiased = 1, kBounded = 2, kCapped = 3 };
+// running maximum (and a bias); the same under a wide cap
+enum { kPlain = 0, kBiased = 1, kBounded = 2, kCapped = 3, kWide = 4 };
+// how the backward undoes it
+enum { kNoCap = 0, kNarrowCap = 1, kWideCap = 2 };
 
 __device__ __attribute__((aligned(16))) const uint32_t kZeroChunk[4] = {0, 0, 0, 0};
 
@@ -325,17 +327,52 @@ __device__ __forceinline__ void fill_nan(float* p, int64_t n) {
 struct Scores {
   float c;             // scale log2(e): z in units of log 2
   float a, b;          // capped: a = cap log2(e); tanh(z / cap) = 1 - 2 / (1 + 2^(b q.k))
+  float t;             // scale / cap
   float ref;           // kBounded: the fixed reference of the exponents
   float slope;         // slope log2(e)
 };
 __device__ __forceinline__ Scores scores_of(const MaskedDims& d, int head, bool biased) {
-  return {d.c, d.cap_a, d.cap_b, d.ref, biased && d.slopes ? d.slopes[head] * kLog2e : 0.0f};
+  return {d.c, d.cap_a, d.cap_b, d.cap_t, d.ref, biased && d.slopes ? d.slopes[head] * kLog2e : 0.0f};
 }
 // from a reference maximum (units of log 2) and the sum of 2^(score - it): -inf where there is no key; a NaN stays one
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : m * kLn2 + logf(l); }
 // 1 / (1 + 2^(b q.k)) = (1 - tanh) / 2
 __device__ __forceinline__ float cap_half(const Scores& sc, float x) {
   return __builtin_amdgcn_rcpf(1.0f + fast_exp2(x * sc.b));
+}
+// Wide caps.  a - 2 a cap_half is a difference of two numbers near a wherever |z| is far below the cap, and off by up to 2^-22 a whatever the
+// score: 2e-5 at a cap of 50, and at one of 1e8 a score of 20 drowns in it.  Up to a = kNarrow (a cap of 709) that is below 2^-12, a
+// sixteenth of the half step to which a probability is rounded next.  Beyond, while |z / cap| < 1/4, the score is z tanh(t) / t, t = z / cap, by
+// the series in t^2 up to t^8 (the next term is 8e-9 at 1/4), and else a (1 - 2 cap_half), which there is good to 16 half-steps of itself.  8192
+// causal tokens, 16 / 8 heads of 128, forward and backward in us: a cap of 100 this way 500 and 1468, the narrow way 371 and 1103; of 1000
+// this way 400 and 1464.
+constexpr float kNarrow = 1024.0f;
+__device__ __forceinline__ float tanh_over(float u) {
+  const float w = (u - 2.4677419f) * (62.0f / 2835.0f);                        // 62/2835 u - 17/315
+  return fmaf(u, fmaf(u, fmaf(u, w, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+}
+// is any of the wavefront's scores beyond?  (a NaN is)
+template <int N>
+__device__ __forceinline__ bool any_far(const Scores& sc, const f32x16 (&x)[N]) {
+  float top = 0.0f;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(x[k][v]));
+  return __any(!(top * sc.t < 0.25f));
+}
+// kFar: some may be beyond.  r: (1 - tanh) / 2
+template <bool kFar>
+__device__ __forceinline__ float wide_score(const Scores& sc, float x, float& r) {
+  const float t = x * sc.t, u = t * t, g = tanh_over(u);
+  float y = x * sc.c * g;
+  r = fmaf(-0.5f * t, g, 0.5f);
+  if constexpr (kFar) {
+    const float far = cap_half(sc, x);
+    r = u < 0.0625f ? r : far;
+    y = u < 0.0625f ? y : sc.a * fmaf(-2.0f, far, 1.0f);
+  }
+  return y;
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------------------------
@@ -383,6 +420,20 @@ __device__ __forceinline__ void masked_block(MaskedState<H>& st, uint32_t k_lds,
 #pragma unroll
   for (int i = 0; i < kFirst; ++i) fetch_v(i);
   __builtin_amdgcn_sched_barrier(0);
+  if constexpr (kMode == kWide) {
+    float r;
+    if (any_far(sc, s)) {
+#pragma unroll
+      for (int i = 0; i < NT * 16; ++i) {
+        float x = s[i / 16][i % 16];
+        asm("" : "+v"(x));             // else what the two branches share is formed for all scores before them: registers
+        s[i / 16][i % 16] = wide_score<true>(sc, x, r);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NT * 16; ++i) s[i / 16][i % 16] = wide_score<false>(sc, s[i / 16][i % 16], r);
+    }
+  }
 #pragma unroll
   for (int kt = 0; kt < NT; ++kt)
 #pragma unroll
@@ -392,7 +443,7 @@ __device__ __forceinline__ void masked_block(MaskedState<H>& st, uint32_t k_lds,
       if constexpr (kMode == kBounded) x = fmaf(-2.0f * sc.a, cap_half(sc, x), sc.a - sc.ref);
       if constexpr (kMode == kCapped) x = fmaf(-2.0f * sc.a, cap_half(sc, x), sc.a);
       if constexpr (kMode == kBiased) x = x * sc.c;
-      if constexpr (kMode == kBiased || kMode == kCapped) x = fmaf(-sc.slope, fabsf(gap - static_cast<float>(j)), x);
+      if constexpr (kMode == kBiased || kMode == kCapped || kMode == kWide) x = fmaf(-sc.slope, fabsf(gap - static_cast<float>(j)), x);
       s[kt][v] = x;
     }
   if (masked) {
@@ -402,7 +453,7 @@ __device__ __forceinline__ void masked_block(MaskedState<H>& st, uint32_t k_lds,
       for (int v = 0; v < 16; ++v)
         s[kt][v] = static_cast<uint32_t>(first + 32 * kt + 8 * (v / 4) + v % 4) < static_cast<uint32_t>(len) ? s[kt][v] : -INFINITY;
   }
-  if constexpr (DH == 128 && (kMode == kBiased || kMode == kCapped)) __builtin_amdgcn_sched_barrier(0);   // registers
+  if constexpr (DH == 128 && (kMode == kBiased || kMode == kCapped || kMode == kWide)) __builtin_amdgcn_sched_barrier(0);   // registers
   if constexpr (kMode != kBounded) {
     float mx = s[0][0];
 #pragma unroll
@@ -540,7 +591,7 @@ k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const b
   const bool causal = tag.w[kTagFlags] & 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
   const int kvh = pair % d.n_kv, head = kvh * (d.n_q / d.n_kv) + pair / d.n_kv;
-  const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped);
+  const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped || kMode == kWide);
 
   const int mine = min(32, rows - 32 * wave);          // this wavefront's queries (none: <= 0)
   const bool live = n < mine;
@@ -643,16 +694,18 @@ k_masked_join_fwd(const int* __restrict__ plan, PlanTag tag, PlanSizes z, Masked
 }
 
 // ---- backward: dq ---------------------------------------------------------------------------------------------------------------
-// x: q.k of an element -> its probability, with `shift` what a query's scores are shifted by (in units of log 2; capped: the cap less
-// lse, else -lse); and a quarter of what the cap leaves of a gradient: with r = (1 - tanh) / 2, 1 - tanh^2 = 4 (r - r^2).  The 4 is in
-// d.grad_scale.
-template <bool kCap, bool kBias>
+// x: q.k of an element -> its probability, with `shift` what a query's scores are shifted by (in units of log 2; under a narrow cap: the cap
+// less lse, else -lse); and a quarter of what the cap leaves of a gradient: with r = (1 - tanh) / 2, 1 - tanh^2 = 4 (r - r^2).  The 4 is
+// in d.grad_scale.
+template <int kCap, bool kBias>
 __device__ __forceinline__ float prob_of(float x, const Scores& sc, float shift, float gap, float& slack) {
   float y;
-  if constexpr (kCap) {
+  if constexpr (kCap == kNarrowCap) {
     const float r = cap_half(sc, x);
     slack = fmaf(-r, r, r);
     y = fmaf(-2.0f * sc.a, r, shift);
+  } else if constexpr (kCap == kWideCap) {             // x is the score already
+    y = x + shift;
   } else {
     y = fmaf(x, sc.c, shift);
   }
@@ -660,9 +713,21 @@ __device__ __forceinline__ float prob_of(float x, const Scores& sc, float shift,
   return fast_exp2(y);
 }
 
+// Wide caps: q.k of a tile become scores, and what the cap leaves of their gradients is multiplied into dP - delta: one after the other, in
+// place, and without a branch for tiles that have none beyond, since that takes 16 registers more than dk and dv of heads of 128 have
+__device__ __forceinline__ void wide_scores(const Scores& sc, f32x16& s, f32x16& dp) {
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    float r;
+    s[v] = wide_score<true>(sc, s[v], r);
+    dp[v] *= fmaf(-r, r, r);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // 32 keys (half kt of the tiles).  The operands from LDS pass through a ring of kRing, each requested kRing - 1 matrix instructions
 // ahead, as in the dk / dv kernel, and for its reason: with all of them requested at once registers run out.
-template <class H, bool kCap, bool kBias>
+template <class H, int kCap, bool kBias>
 __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x8 (&qf)[H::KS], const bf16x8 (&dof)[H::KS], float shift,
                                                const f32x16& less, uint32_t k_rows, uint32_t v_rows, uint32_t k_cols, const Scores& sc, bool last, bool masked,
                                                int first, int len, float gap) {
@@ -685,13 +750,14 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
     s = mfma(f[(2 * KS - 2) % kRing], qf[KS - 1], s);
     dp = mfma(f[(2 * KS - 1) % kRing], dof[KS - 1], dp);
   }
+  if constexpr (kCap == kWideCap) wide_scores(sc, s, dp);
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const int j = 8 * (v / 4) + v % 4;
     float slack = 1.0f;
     float p = prob_of<kCap, kBias>(s[v], sc, shift, gap - static_cast<float>(j), slack);
     dp[v] *= p;
-    if constexpr (kCap) dp[v] *= slack;
+    if constexpr (kCap == kNarrowCap) dp[v] *= slack;
   }
   if (masked) {
 #pragma unroll
@@ -713,7 +779,7 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
 // The forward's split, walked again: S and dP = V dO^T in tiles of 32 keys, dq^T += K^T dz^T.  Bound like the forward, by a query's four operands
 // on short sequences: 8192 causal tokens, 16 / 8 heads of 128, 375 us (scores of deviation 1) to 428 (9), 485 capped; 24 documents
 // of 8192 tokens 71, of which vector unit 27 and matrix cores 13.
-template <class H, bool kCap, bool kBias>
+template <class H, int kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                 const bf16_t* __restrict__ O, const uint8_t* __restrict__ o_low, const float* __restrict__ lse, const int* __restrict__ plan, PlanTag tag,
@@ -773,7 +839,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
   }
   dl = half_sum(dl);
   if (live) {
-    shift = (kCap ? sc.a : 0.0f) - lse0 * kLog2e;
+    shift = (kCap == kNarrowCap ? sc.a : 0.0f) - lse0 * kLog2e;
     if (hi == 0) {
       delta[(int64_t)head * d.Tq + t0] = -dl;
       delta[((int64_t)d.n_q + head) * d.Tq + t0] = shift;
@@ -823,7 +889,7 @@ k_masked_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, cons
 // ---- backward: dk, dv -----------------------------------------------------------------------------------------------------------
 // 32 queries x 32 keys; registers and rings as in the causal kernel.  first: index of the lane's first query relative to the first that
 // sees the lane's key, of `len`; gap: distance of the lane's key from the lane's first query.
-template <class H, bool kCap, bool kBias>
+template <class H, int kCap, bool kBias>
 __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv)[H::DT], const bf16x8 (&kf)[H::KS],
                                                 const bf16x8 (&vf)[H::KS], const float* shift_lds, const float* delta_lds, uint32_t q_rows,
                                                 uint32_t q_cols, const Scores& sc, bool last, bool masked, int first, int len, float gap, int lane) {
@@ -852,6 +918,7 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
     s = mfma(f[(2 * KS - 2) % kRing], kf[KS - 1], s);
     dp = mfma(f[(2 * KS - 1) % kRing], vf[KS - 1], dp);
   }
+  if constexpr (kCap == kWideCap) wide_scores(sc, s, dp);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int row = 8 * j + 4 * (lane >> 5);
@@ -863,7 +930,7 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
       float p = prob_of<kCap, kBias>(s[4 * j + r], sc, lr[r], gap + static_cast<float>(8 * j + r), slack);
       s[4 * j + r] = p;
       float g = p * dp[4 * j + r];
-      if constexpr (kCap) g *= slack;
+      if constexpr (kCap == kNarrowCap) g *= slack;
       dp[4 * j + r] = g;
     }
     if (j == 1 || kBias) __builtin_amdgcn_sched_barrier(0);
@@ -894,7 +961,7 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
 // block of 64 and 2, 3 the others, and the two sums of a block of keys meet through LDS at the end.  All query heads of the group are walked,
 // so that no sum leaves the workgroup.  K, V, dk and dv take the registers of two wavefronts a SIMD (three with heads of 64: 13 images of
 // 10007 patches 153 us, with two 172).  8192 causal tokens, 16 / 8 heads of 128: 528 us (scores of deviation 1) to 633 (9), 645 capped.
-template <class H, bool kCap, bool kBias>
+template <class H, int kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                  const float* __restrict__ delta, const int* __restrict__ plan, PlanTag tag, PlanSizes z, MaskedDims d,
@@ -1083,7 +1150,7 @@ k_masked_token(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const
   const int seq = w.item(0), row0 = w.item(1), keys = w.item(2), gap0 = w.item(3), pieces = w.item(4);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hi = lane >> 5;
   const int heads = min(32, rep - h0), head = kvh * rep + h0 + min(n, heads - 1);
-  const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped);
+  const Scores sc = scores_of(d, head, kMode == kBiased || kMode == kCapped || kMode == kWide);
 
   MaskedState<H> st;
 #pragma unroll
@@ -1284,7 +1351,7 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
   // A capped score is at most a = cap log2(e): with exponents from 2^-110 (reference a - 110 at least, so that none is lost) to
   // 2^40 (a <= 75) sums of 2^20 of them with any sensible value stay in range, and no running maximum is needed (8192 causal tokens, 16 / 8
   // heads of 128: 390 us without, 406 with).
-  const int mode = d.cap_a > 0.0f ? (!d.slopes && d.cap_a <= 75.0f ? kBounded : kCapped) : d.slopes ? kBiased : kPlain;
+  const int mode = d.cap_a > kNarrow ? kWide : d.cap_a > 0.0f ? (!d.slopes && d.cap_a <= 75.0f ? kBounded : kCapped) : d.slopes ? kBiased : kPlain;
   const int rep = d.n_q / d.n_kv;
   const int64_t cols = (int64_t)d.n_kv * ((rep + 31) / 32);
   const dim3 grid(static_cast<unsigned>(single ? z.max_q * cols : z.max_q * d.n_q));
@@ -1300,7 +1367,8 @@ hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, 
     case kPlain: FAAR_MF(kPlain); break;
     case kBiased: FAAR_MF(kBiased); break;
     case kBounded: FAAR_MF(kBounded); break;
-    default: FAAR_MF(kCapped); break;
+    case kCapped: FAAR_MF(kCapped); break;
+    default: FAAR_MF(kWide); break;
   }
 #undef FAAR_MF
 #undef FAAR_MF2
@@ -1326,8 +1394,9 @@ hipError_t launch_masked_bwd(const bf16_t* dO, const bf16_t* Q, const bf16_t* K,
   } while (0)
 #define FAAR_MB(C, B) \
   do { if (d.dh <= 64) FAAR_MB2(Heads64, C, B); else if (d.dh <= 96) FAAR_MB2(Heads96, C, B); else FAAR_MB2(Heads128, C, B); } while (0)
-  if (d.cap_a > 0.0f) { if (d.slopes) FAAR_MB(true, true); else FAAR_MB(true, false); }
-  else                { if (d.slopes) FAAR_MB(false, true); else FAAR_MB(false, false); }
+  if (d.cap_a > kNarrow) FAAR_MB(kWideCap, true);
+  else if (d.cap_a > 0.0f) { if (d.slopes) FAAR_MB(kNarrowCap, true); else FAAR_MB(kNarrowCap, false); }
+  else                     { if (d.slopes) FAAR_MB(kNoCap, true); else FAAR_MB(kNoCap, false); }
 #undef FAAR_MB
 #undef FAAR_MB2
   if (hipError_t e = hipGetLastError()) return e;
