@@ -676,9 +676,9 @@ int faar_rope_axes(const void* q, int64_t ldq, int64_t n_q, const void* k, int64
  *
  * Lengths live on the device and are read there.  A plan is made from them once for a batch (once a token where tokens are generated)
  * and read by the calls of every layer with the same description of rows, heads and mask.  On the device every call looks whether the
- * plan is of its description; if not, or if the plan met a sequence that reaches outside 0 .. Tq / Tk, a negative prefix, or more
- * query rows in all than there are, the call's outputs are NaN throughout.  Key rows may belong to several sequences in the forward
- * (a shared prompt); in the backward no row may (NaN, where the lengths add up to more rows than there are; else undefined).
+ * plan is of its description; if not, or if the plan met a sequence that reaches outside 0 .. Tq / Tk, a negative prefix, or a
+ * query row of several sequences, the call's outputs are NaN throughout.  Key rows may belong to several sequences in the forward (a
+ * shared prompt); a backward over such a plan gives NaN throughout.  Sequences may come in any order.
  *
  * One token a sequence (answering): q_start and q_len NULL.  Query row b is then the last position of sequence b, Tq = n_seq, and the
  * forward splits the caches into pieces that it joins at the end.  There is no backward of this form.
