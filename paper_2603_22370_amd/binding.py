@@ -251,8 +251,10 @@ def _row_stride(t, rows, width, where):
     return max(ld, width) if rows == 1 else ld
 
 
-def _whole(t, dtype, numel, where):
-    """A contiguous device tensor of that type and size."""
+def _whole(t, dtype, numel, where, width=None):
+    """A contiguous device tensor of that type and size (and row length)."""
+    if width is not None and (t.dim() == 0 or t.shape[-1] != width):
+        raise ValueError(f"{where}: a tensor is {tuple(t.shape)}, not rows of {width}")
     if t.dtype is not dtype or t.numel() != numel or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{where}: a contiguous {dtype} device tensor of {numel} entries is wanted")
 
@@ -645,7 +647,7 @@ def faar_layernorm_bwd(dh1, x, g, mean, rstd, dh2=None, d_res=None, dh3=None, wa
     _whole(x, _BF16 if x.dtype is _BF16 else _F32, T * D, where)
     for t in (dh1, dh2, dh3, d_res):
         if t is not None:
-            _whole(t, _BF16, T * D, where)
+            _whole(t, _BF16, T * D, where, D)
     _whole(g, _F32, D, where)
     _whole(mean, _F32, T, where)
     _whole(rstd, _F32, T, where)
@@ -789,9 +791,9 @@ def _masked_call(a, where, plan, q, k, v, o, stats, ws):
     d.ldq, d.ldk, d.ldv, d.ldo = (_row_stride(q, Tq, qd, where), _row_stride(k, Tk, kd, where), _row_stride(v, Tk, kd, where),
                                   _row_stride(o, Tq, qd, where))
     if stats is not None:
-        _whole(stats.lse, _F32, a.n_q * Tq, where)
+        _whole(stats.lse, _F32, a.n_q * Tq, where, Tq)
         if stats.o_low is not None:
-            _whole(stats.o_low, torch.int8, Tq * qd, where)
+            _whole(stats.o_low, torch.int8, Tq * qd, where, qd)
     _dev(plan, ws)
     return d
 
