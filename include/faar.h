@@ -685,7 +685,9 @@ int faar_rope_axes(const void* q, int64_t ldq, int64_t n_q, const void* k, int64
  */
 enum { FAAR_ATTENTION_CAUSAL = 1 };
 typedef struct {
-  int64_t n_seq;           /* sequences, at most 2^20 */
+  int64_t n_seq;           /* sequences, at most 2^20; FAAR_E_SHAPE where a launch would need 2^32 threads: (Tq / 128 + n_seq) n_q or, in the
+                              backward, (Tk / 64 + n_seq) n_kv near 2^24; single tokens: n_seq n_kv (of every 32 query heads) near 2^24
+                              or n_seq n_q of 2^25 */
   int64_t Tq, Tk;          /* rows of q, o and of k, v: at most 2^30 */
   const int32_t* q_start;  /* in  device int32[n_seq]; q_start and q_len both NULL: one token a sequence */
   const int32_t* q_len;

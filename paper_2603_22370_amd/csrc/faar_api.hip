@@ -1000,7 +1000,9 @@ struct MaskedCall {
   bool single;
 };
 
-int masked_call(const faar_attention* a, MaskedCall& c) {
+constexpr int64_t kMaxThreads = 0xFFFFFFFFLL;
+
+int masked_call(const faar_attention* a, MaskedCall& c, bool backward) {
   if (!a) return FAAR_E_NULL;
   c.single = !a->q_start && !a->q_len;
   if ((!a->q_start) != (!a->q_len) || (!a->k_start) != (!a->k_len) || (c.single && !a->k_start)) return FAAR_E_NULL;
@@ -1015,8 +1017,10 @@ int masked_call(const faar_attention* a, MaskedCall& c) {
     if (reinterpret_cast<uintptr_t>(p) & 3u) return FAAR_E_ARG;
   if (reinterpret_cast<uintptr_t>(a->slopes) & 3u) return FAAR_E_ARG;
   c.z = attention_plan_sizes(a->n_seq, a->Tq, a->Tk, a->n_q, a->n_kv, c.single);
-  // the largest grids: work items x heads, and for single tokens one query head of a sequence each
-  if (c.z.max_q * a->n_q > 0x7FFFFFFFLL || c.z.max_k * 2 * a->n_kv > 0x7FFFFFFFLL || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
+  // the largest grids (a launch has below 2^32 threads): work items x heads, and for single tokens one query head of a sequence each
+  const int64_t groups = c.single ? a->n_kv * ((a->n_q / a->n_kv + 31) / 32) : a->n_q;
+  if (c.z.max_q * groups * 256 > kMaxThreads || (c.single && a->Tq * a->n_q * 128 > kMaxThreads) || c.z.words > 0x7FFFFFFFLL) return FAAR_E_SHAPE;
+  if (backward && !c.single && c.z.max_k * a->n_kv * 256 > kMaxThreads) return FAAR_E_SHAPE;
   const int window = a->window >= kMaxRows ? 0 : static_cast<int>(a->window);    // no two positions are that far apart: none
   const int tag[kPlanTagWords] = {0x5A11FAA3, static_cast<int>(a->flags) | (c.single ? 2 : 0), static_cast<int>(a->n_seq), static_cast<int>(a->Tq),
                                   static_cast<int>(a->Tk), window, static_cast<int>(a->n_q), static_cast<int>(a->n_kv)};
@@ -1047,19 +1051,19 @@ size_t masked_ws_bytes(const MaskedCall& c, bool backward) {
 
 size_t faar_attention_plan_bytes(const faar_attention* a) {
   MaskedCall c;
-  return masked_call(a, c) == FAAR_OK ? align256((size_t)c.z.words * 4) : 0;
+  return masked_call(a, c, false) == FAAR_OK ? align256((size_t)c.z.words * 4) : 0;
 }
 
 size_t faar_attention_masked_workspace_bytes(const faar_attention* a, int32_t backward) {
   MaskedCall c;
-  if (masked_call(a, c) != FAAR_OK || (backward && c.single)) return 0;
+  if (masked_call(a, c, backward != 0) != FAAR_OK || (backward && c.single)) return 0;
   return masked_ws_bytes(c, backward != 0);
 }
 
 int faar_attention_plan(const faar_attention* a, void* plan, size_t plan_bytes, void* stream) {
   if (!a || !plan) return FAAR_E_NULL;
   MaskedCall c;
-  if (int e = masked_call(a, c)) return e;
+  if (int e = masked_call(a, c, false)) return e;
   if (!aligned16(plan)) return FAAR_E_ARG;
   if (plan_bytes < align256((size_t)c.z.words * 4)) return FAAR_E_WORKSPACE;
   return hip_status(launch_attention_plan(a->q_start, a->q_len, a->k_start ? a->k_start : a->q_start, a->k_len ? a->k_len : a->q_len, a->prefix,
@@ -1070,7 +1074,7 @@ int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t 
                               float* lse, uint8_t* o_low, void* ws, size_t ws_bytes, void* stream) {
   if (!a || !plan || !q || !k || !v || !o) return FAAR_E_NULL;
   MaskedCall c;
-  if (int e = masked_call(a, c)) return e;
+  if (int e = masked_call(a, c, false)) return e;
   if (c.single && o_low) return FAAR_E_UNSUPPORTED;
   if (int e = masked_rows(a)) return e;
   if (!aligned16(plan) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_low) || !aligned16(ws) ||
@@ -1088,7 +1092,7 @@ int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t 
                               size_t ws_bytes, void* stream) {
   if (!a || !plan || !d_o || !q || !k || !v || !o || !lse || !dq || !dk || !dv) return FAAR_E_NULL;
   MaskedCall c;
-  if (int e = masked_call(a, c)) return e;
+  if (int e = masked_call(a, c, true)) return e;
   if (c.single) return FAAR_E_UNSUPPORTED;
   if (int e = masked_rows(a)) return e;
   for (const void* p : {plan, d_o, q, k, v, o, static_cast<const void*>(o_low), static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(ws)})
