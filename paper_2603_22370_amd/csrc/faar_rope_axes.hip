@@ -24,7 +24,8 @@ __global__ void __launch_bounds__(kEltThreads)
 k_rope_axes(RopeTensor q, RopeTensor k, int64_t T, int dh, int half, const int32_t* __restrict__ pos, RopeAxes ax, float sign, bool pairs,
             bool copy_rest) {
   __shared__ __attribute__((aligned(16))) float cs[TB][2][kRopeMaxHalf];   // [token][cos, sin][frequency]
-  const int64_t t0 = blockIdx.x * (int64_t)TB;
+  const int64_t t0 = (blockIdx.y * (int64_t)gridDim.x + blockIdx.x) * TB;
+  if (t0 >= T) return;
   const int nt = static_cast<int>(T - t0 < TB ? T - t0 : TB);
   for (int i = threadIdx.x; i < nt * half; i += kEltThreads) {
     const int t = i / half, f = i - t * half;
@@ -83,8 +84,10 @@ hipError_t launch_rope_axes(const RopeTensor& q, const RopeTensor& k, int64_t T,
   // four tokens a workgroup give each of its threads one sine at 64 frequencies; few tokens spread over the device one by one.  One / four
   // a workgroup, 16 + 8 heads of 128 and 8 + 8 of 64 taken together, in us: 64 tokens 3.6 / 4.5, 512 4.1 / 5.1, 2048 6.6 / 6.6,
   // 8192 18.0 / 15.4, 40000 97 / 87
+  constexpr int64_t kRow = 1 << 23;                    // workgroups of a grid's row: a row has below 2^32 threads
+  const int64_t n = (T + 3) / 4;
   if (T >= 2048)
-    hipLaunchKernelGGL(k_rope_axes<4>, dim3(static_cast<unsigned>((T + 3) / 4)), dim3(kEltThreads), 0, st, q, k, T, dh, half, pos, ax, sign, pairs, copy_rest);
+    hipLaunchKernelGGL(k_rope_axes<4>, dim3(static_cast<unsigned>(n < kRow ? n : kRow), static_cast<unsigned>((n + kRow - 1) / kRow)), dim3(kEltThreads), 0, st, q, k, T, dh, half, pos, ax, sign, pairs, copy_rest);
   else
     hipLaunchKernelGGL(k_rope_axes<1>, dim3(static_cast<unsigned>(T)), dim3(kEltThreads), 0, st, q, k, T, dh, half, pos, ax, sign, pairs, copy_rest);
   return hipGetLastError();
