@@ -699,7 +699,7 @@ typedef struct {
   int64_t n_q, n_kv, dh;   /* n_q % n_kv == 0; dh a multiple of 8, at most 128 */
   int64_t ldq, ldk, ldv, ldo; /* elements between rows of q (and dq), k (dk), v (dv), o (d_o): multiples of 8, heads side by side in a
                                  row; q, k and v may be parts of one buffer, and so may their gradients */
-  float scale;             /* > 0, at most 2^126 */
+  float scale;             /* > 0, at most 2^126 (with a cap 2^125) */
   float cap;               /* 0: none; of any size: what it costs a score of its float32 digits is below 2^-12 */
   const float* slopes;     /* in  device float[n_q], nullable: finite */
 } faar_attention;

@@ -1027,7 +1027,7 @@ int masked_call(const faar_attention* a, MaskedCall& c, bool backward) {
   for (int i = 0; i < kPlanTagWords; ++i) c.tag.w[i] = tag[i];
   constexpr float kL2e = 1.4426950408889634f;
   const float cap_a = a->cap * kL2e, cap_b = a->cap > 0.0f ? 2.0f * kL2e * a->scale / a->cap : 0.0f;
-  if (!std::isfinite(cap_a) || !std::isfinite(cap_b) || a->scale > 0x1p126f) return FAAR_E_ARG;
+  if (!std::isfinite(cap_a) || !std::isfinite(cap_b) || a->scale > (a->cap > 0.0f ? 0x1p125f : 0x1p126f)) return FAAR_E_ARG;   // dq, dk: 4 scale
   c.d = MaskedDims{static_cast<int>(a->n_q), static_cast<int>(a->n_kv), static_cast<int>(a->dh), a->Tq, a->Tk, a->ldq, a->ldk, a->ldv, a->ldo,
                    a->cap > 0.0f ? 4.0f * a->scale : a->scale, a->scale * kL2e, cap_a, cap_b,
                    a->cap > 0.0f ? a->scale / a->cap : 0.0f, std::min(cap_a, 110.0f - cap_a), a->slopes};

@@ -47,3 +47,11 @@ def test_grids_of_more_threads_than_a_launch_has():
     single = dict(q_start=None, q_len=None, k_start=0x1000, k_len=0x1000, n_seq=n, Tq=n, Tk=1 << 30)
     assert plan_bytes(description(n_q=16, n_kv=1, **single)) > 0 and plan_bytes(description(n_q=8, n_kv=8, **single)) > 0
     assert refused(description(n_q=32, n_kv=1, **single)) and refused(description(n_q=16, n_kv=16, **single))
+
+
+def test_scales_whose_gradients_would_overflow():
+    """Under a cap dq and dk are sums times 4 scale: at 2^126 that is infinite."""
+    for scale, cap, fits in ((2.0 ** 126, 0.0, True), (2.0 ** 126, 50.0, False), (2.0 ** 125, 50.0, True), (2.0 ** 125, 1e30, True), (2.0 ** 126, 1e30, False)):
+        a = description(scale=scale, cap=cap)
+        assert (plan_bytes(a) > 0) == fits and (workspace(a, 1) > 0) == fits, (scale, cap)
+        assert fits or fb.lib().faar_attention_plan(ctypes.byref(a), P, BIG, NUL) == -6
