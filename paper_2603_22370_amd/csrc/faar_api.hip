@@ -1102,6 +1102,7 @@ int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t 
   for (const void* out : {dq, dk, dv})
     for (const void* in : {d_o, q, k, v, o})
       if (out == in) return FAAR_E_ARG;
+  if (dq == dk || dq == dv || dk == dv) return FAAR_E_ARG;
   return hip_status(launch_masked_bwd(static_cast<const bf16_t*>(d_o), static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(k),
                                       static_cast<const bf16_t*>(v), static_cast<const bf16_t*>(o), o_low, lse, static_cast<const int*>(plan), c.tag,
                                       c.z, c.d, static_cast<float*>(ws), static_cast<bf16_t*>(dq), static_cast<bf16_t*>(dk), static_cast<bf16_t*>(dv),

@@ -55,3 +55,11 @@ def test_scales_whose_gradients_would_overflow():
         a = description(scale=scale, cap=cap)
         assert (plan_bytes(a) > 0) == fits and (workspace(a, 1) > 0) == fits, (scale, cap)
         assert fits or fb.lib().faar_attention_plan(ctypes.byref(a), P, BIG, NUL) == -6
+
+
+def test_gradients_in_one_place_are_refused():
+    a = description(dh=64)
+    at = [ctypes.c_void_p(0x100000 * (i + 1)) for i in range(12)]
+    plan, d_o, q, k, v, o, lse, ws = at[:8]
+    for dq, dk, dv in ((at[8], at[8], at[9]), (at[8], at[9], at[8]), (at[8], at[9], at[9])):
+        assert fb.lib().faar_attention_masked_bwd(ctypes.byref(a), plan, BIG, d_o, q, k, v, o, lse, NUL, dq, dk, dv, ws, BIG, NUL) == -6
