@@ -733,7 +733,7 @@ def attention_description(n_q, n_kv, dh, Tq, Tk, start, length, k_start=None, k_
     """A faar_attention for the calls below (see faar.h).  start, length: int32 device tensors [n_seq], the rows of each sequence in q, and
     in k and v where k_start, k_len do not say otherwise; single: one token a sequence, start and length are those of the caches.
     Keeps references to every tensor it points to."""
-    if single and k_start is not None:
+    if single and (k_start is not None or k_len is not None):
         raise ValueError("attention_description: the sequences of single tokens are those of the caches")
     q = (None, None) if single else (start, length)
     k = (start, length) if single else (k_start, k_len)

@@ -30,3 +30,10 @@ def test_rows_of_another_length_are_refused():
     for lse, low, width in ((stats.lse.t().contiguous(), stats.o_low, "rows of 24"), (stats.lse, stats.o_low.t().contiguous(), "rows of 128")):
         with pytest.raises(ValueError, match=width):
             faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, faar.AttentionStats(lse, low))
+
+
+def test_lengths_of_their_own_for_caches_of_single_tokens_are_refused():
+    n = torch.ones(2, dtype=torch.int32)
+    for kw in (dict(k_start=n), dict(k_len=n), dict(k_start=n, k_len=n)):
+        with pytest.raises(ValueError, match="those of the caches"):
+            faar.attention_description(2, 1, 64, 2, 64, n, n, single=True, **kw)
