@@ -1383,8 +1383,9 @@ hipError_t launch_attention_plan(const int* q_start, const int* q_len, const int
 hipError_t launch_masked_fwd(const bf16_t* Q, const bf16_t* K, const bf16_t* V, const int* plan, const PlanTag& tag, const PlanSizes& z,
                              const MaskedDims& d, bool single, bf16_t* O, float* lse, uint8_t* o_low, float* part, hipStream_t st) {
   // A capped score is at most a = cap log2(e): with exponents from 2^-110 (reference a - 110 at least, so that none is lost) to
-  // 2^40 (a <= 75) sums of 2^20 of them with any sensible value stay in range, and no running maximum is needed (8192 causal tokens, 16 / 8
-  // heads of 128: 390 us without, 406 with).
+  // 2^40 (a <= 75) sums of 2^20 of them with values of up to 2^60 stay in range, and at the low end, where all of a row's scores are -cap,
+  // products end at 2^-149, 2^-39 of v's unit; so no running maximum is needed (8192 causal tokens, 16 / 8 heads of 128: 390 us
+  // without, 406 with).
   const int mode = d.cap_a > kNarrow ? kWide : d.cap_a > 0.0f ? (!d.slopes && d.cap_a <= 75.0f ? kBounded : kCapped) : d.slopes ? kBiased : kPlain;
   const int rep = d.n_q / d.n_kv;
   const int64_t cols = (int64_t)d.n_kv * ((rep + 31) / 32);

@@ -8,7 +8,7 @@ a score nothing of its own precision.  P and ds are rounded to bf16, and so is e
     o:   U8 |o| + (U8 + 2 e) sum P |v|
     dv:  U8 |dv| + sum (U8 + 2 e) P |dO|
     dq, dk:  U8 |.| + scale sum |k| (or |q|) times the error of dz = P (dP - delta) slack, which is (U8 + 4 e) |dz|, 22 u P |dP - delta| of the slack
-         (4 r (1 - r), r good to 5 u) and P slack times what dP and delta are off by: u 2 dh sum |dO| |v| and for delta
+         (4 r (1 - r), r good to 5 u), P slack times what dP and delta are off by, and the product of the two errors: u 2 dh sum |dO| |v| and for delta
       without the low bytes of o   sum |dO| tol(o)
       with them                    1.02 (U8 + 2 e) sum P |dP - delta| + 2^-15 sum |dO| |o| + (64 + n / 16) u sum |dO| sum P |v|
     since then o = sum w v / sum w with w = P (1 + eps), |eps| <= U8 + 2 e, so that o is off by sum P eps (v - o) up to second order, by what
@@ -72,7 +72,8 @@ def bounds(q, k, v, seqs, n_q, n_kv, dh, scale, causal=True, window=0, cap=0.0, 
                 off = off + 1.02 * eps * raw.sum(axis=1, keepdims=True) + (np.abs(do) * stored).sum(axis=1, keepdims=True)
             else:
                 off = off + (np.abs(do) * tol["o"][rows, cq]).sum(axis=1, keepdims=True)
-            dz = (U8 + 4 * e) * raw * slack + P * slack * off + (22 * U * raw if cap else 0.0)
+            # with the slack off by t <= 22 u and dP - delta by d <= off: (x + d) (slack + t) - x slack = x t + slack d + t d
+            dz = (U8 + 4 * e) * raw * slack + P * slack * off + (22 * U * (raw + P * off) if cap else 0.0)
             tol["dq"][rows, cq] += scale * (dz @ np.abs(kh))
             tol["dk"][keys, ck] += scale * (dz.T @ np.abs(qh))
             tol["dv"][keys, ck] += (eps * P).T @ np.abs(do)
@@ -189,3 +190,52 @@ def test_norms_of_errors(name):
 def test_long_sequences(name, seqs, n_q, n_kv, dh, more):
     c = Case(seqs, n_q, n_kv, dh, **more)
     forward_and_backward(c, *bounds_of(c))
+
+
+def saturated(seqs, n_q, n_kv, dh, cap, **more):
+    """Scores of +-cap: rows of q whose scores are all -cap and rows whose are all +cap in turn, every seventh with scores in between.  Columns of
+    v from 2^-18 up to 2^9."""
+    c = Case(seqs, n_q, n_kv, dh, cap=cap, **more)
+    rng = np.random.default_rng([int(cap), dh])
+    way = bf(rng.standard_normal(dh))
+    size = 16.0 * cap / (c.scale * float((way * way).sum()))             # |z / cap| is 12 and more: tanh is 1 to 1e-10
+    sign = np.where(np.arange(c.Tq) % 2 == 0, -1.0, 1.0)
+    sign[np.arange(c.Tq) % 7 == 3] = 0.0
+    c.q = np.tile(bf(size * sign[:, None] * way[None, :]), (1, n_q))
+    loose = sign == 0.0
+    c.q[loose] = bf(rng.standard_normal((int(loose.sum()), n_q * dh)) * 4.0)
+    c.k = np.tile(bf(way[None, :] * rng.uniform(0.75, 1.25, (c.Tk, 1))), (1, n_kv))
+    c.v = bf(c.v * np.tile(2.0 ** (np.arange(dh) * 28 // dh - 18.0), n_kv)[None, :])
+    return c
+
+
+ENDS = {"packed": (packed([130, 64, 1, 200], gap=1), 2, 2, 64, {}), "whole_128": (packed([90, 129]), 2, 1, 128, dict(causal=False)),
+        "heads_of_80": (packed([150]), 1, 1, 80, {}), "in_pieces": (packed([1300, 33]), 1, 1, 64, {})}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cap", [50.0, 51.9, 52.1, 30.0])
+@pytest.mark.parametrize("name", list(ENDS))
+def test_scores_at_both_ends_of_their_cap(name, cap):
+    """Up to a cap of 52 exponents have a fixed reference: a row whose scores are all -cap sums terms of 2^-110, and of +cap of 2^40."""
+    seqs, n_q, n_kv, dh, more = ENDS[name]
+    c = saturated(seqs, n_q, n_kv, dh, cap, **more)
+    want, tol = bounds_of(c, both=c.Tq < 1000)
+    o, stats, _ = forward_and_backward(c, want, tol)
+    if c.Tq < 1000:
+        top = o.view(torch.int16).to(torch.int32) << 16
+        whole = (top + (stats.o_low.to(torch.int32) << 8)).view(torch.float32)
+        inside(host(whole)[c.q_rows], want[0][c.q_rows], tol["both"][c.q_rows], "o and its low bytes")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cap", [50.0, 51.9])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_single_tokens_at_both_ends_of_their_cap(cap, dh):
+    rows, lens, n_q = 900, [800, 3, 130, 700], 2
+    c = saturated([(b, 1, b * rows, n, 0) for b, n in enumerate(lens)], n_q, 1, dh, cap, same=False, Tk=4 * rows)
+    want, tol = bounds(c.q, c.k, c.v, c.seqs, n_q, 1, dh, c.scale, cap=cap)
+    a = faar.attention_description(n_q, 1, dh, 4, 4 * rows, ints(b * rows for b in range(4)), ints(lens), single=True, cap=cap)
+    o, stats = faar.faar_attention_masked_fwd(a, faar.faar_attention_plan(a), dev(c.q), dev(c.k), dev(c.v))
+    inside(host(o), want[0], tol["o"], "o")
+    inside(host(stats.lse), want[1], tol["lse"], "lse")
