@@ -239,3 +239,18 @@ def test_single_tokens_at_both_ends_of_their_cap(cap, dh):
     o, stats = faar.faar_attention_masked_fwd(a, faar.faar_attention_plan(a), dev(c.q), dev(c.k), dev(c.v))
     inside(host(o), want[0], tol["o"], "o")
     inside(host(stats.lse), want[1], tol["lse"], "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dh", [64, 128])
+def test_a_nan_stays_one_under_a_wide_cap(dh):
+    c = Case(packed([150, 70]), 2, 1, dh, cap=1e4)
+    a, (q, k, v, d_o) = c.device()
+    plan = faar.faar_attention_plan(a)
+    q[100, dh + 5] = float("nan")
+    o, stats = faar.faar_attention_masked_fwd(a, plan, q, k, v)
+    dq, _, _ = faar.faar_attention_masked_bwd(a, plan, d_o, q, k, v, o, stats)
+    for t in (o, dq):
+        bad = torch.isnan(t).view(-1, 2, dh)
+        assert bool(bad[100, 1].all()) and int(bad.sum()) == dh
+    assert bool(torch.isnan(stats.lse[1, 100])) and int(torch.isnan(stats.lse).sum()) == 1
