@@ -379,7 +379,7 @@ __device__ __forceinline__ float cap_half(const Scores& sc, float x) {
 // sixteenth of the half step to which a probability is rounded next.  Beyond, while |z / cap| < 1/4, the score is z tanh(t) / t, t = z / cap, by
 // the series in t^2 up to t^8 (the next term is 8e-9 at 1/4), and else a (1 - 2 cap_half), which there is good to 16 half-steps of itself.  8192
 // causal tokens, 16 / 8 heads of 128, forward and backward in us: a cap of 100 this way 500 and 1468, the narrow way 371 and 1103; of 1000
-// this way 400 and 1464.
+// this way 399 and 1389 (heads of 64: 271 and 891, the narrow way 285 and 674).
 constexpr float kNarrow = 1024.0f;
 __device__ __forceinline__ float tanh_over(float u) {
   const float w = (u - 2.4677419f) * (62.0f / 2835.0f);                        // 62/2835 u - 17/315
@@ -748,12 +748,20 @@ __device__ __forceinline__ float prob_of(float x, const Scores& sc, float shift,
 }
 
 // Wide caps: q.k of a tile become scores, and what the cap leaves of their gradients is multiplied into dP - delta: one after the other, in
-// place, and without a branch for tiles that have none beyond, since that takes 16 registers more than dk and dv of heads of 128 have
+// place.  kLook: a tile that has no score beyond leaves the exponentials out (dk and dv of heads of 128 lack the registers to look)
+template <bool kLook>
 __device__ __forceinline__ void wide_scores(const Scores& sc, f32x16& s, f32x16& dp) {
+  const bool far = !kLook || any_far(sc, reinterpret_cast<const f32x16(&)[1]>(s));
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
-    float r;
-    s[v] = wide_score<true>(sc, s[v], r);
+    float r, x = s[v];
+    if (far) {
+      if constexpr (kLook) asm volatile("" : "+v"(x));   // keeps what the branches share from being formed for all scores before them
+      x = wide_score<true>(sc, x, r);
+    } else {
+      x = wide_score<false>(sc, x, r);
+    }
+    s[v] = x;
     dp[v] *= fmaf(-r, r, r);
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -784,7 +792,7 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
     s = mfma(f[(2 * KS - 2) % kRing], qf[KS - 1], s);
     dp = mfma(f[(2 * KS - 1) % kRing], dof[KS - 1], dp);
   }
-  if constexpr (kCap == kWideCap) wide_scores(sc, s, dp);
+  if constexpr (kCap == kWideCap) wide_scores<true>(sc, s, dp);
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const int j = 8 * (v / 4) + v % 4;
@@ -952,7 +960,7 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
     s = mfma(f[(2 * KS - 2) % kRing], kf[KS - 1], s);
     dp = mfma(f[(2 * KS - 1) % kRing], vf[KS - 1], dp);
   }
-  if constexpr (kCap == kWideCap) wide_scores(sc, s, dp);
+  if constexpr (kCap == kWideCap) wide_scores<(KS < 8)>(sc, s, dp);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int row = 8 * j + 4 * (lane >> 5);
