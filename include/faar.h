@@ -721,7 +721,7 @@ int faar_attention_masked_fwd(const faar_attention* a, const void* plan, size_t 
                               float* lse, uint8_t* o_low, void* ws, size_t ws_bytes, void* stream);
 
 /* (dq, dk, dv) for the output gradient d_o; o, lse and o_low from the forward call.  o_low may be NULL: the gradients of queries whose
- * softmax is sharp then carry the rounding of o, many times over.  dk and dv are summed over the query heads of a group in a fixed
+ * softmax is sharp then carry the rounding of o, many times over.  P and ds (1 - tanh^2) are rounded to bf16 as matrix-core operands.  dk and dv are summed over the query heads of a group in a fixed
  * order.  Outputs must overlap neither inputs nor one another (FAAR_E_ARG where two start at the same place). */
 int faar_attention_masked_bwd(const faar_attention* a, const void* plan, size_t plan_bytes, const void* d_o, const void* q, const void* k,
                               const void* v, const void* o, const float* lse, const uint8_t* o_low, void* dq, void* dk, void* dv, void* ws,

@@ -62,8 +62,8 @@ __device__ __forceinline__ void store4_bf16(bf16_t* p, float a, float b, float c
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
 }
 
-// 2^x by the hardware instruction alone: the arguments here are at most a few units above zero and results far below one
-// may flush to zero
+// 2^x by the hardware instruction alone: results below 2^-126 may flush to zero, and above 2^128 they are infinite (under a cap, of which the
+// reciprocal is taken; exponents of probabilities stay within a few units of zero, or 40 against a fixed reference)
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // 16 bytes (4 in the second form) per lane from global memory straight into LDS at lds_addr + 16 * lane (4 * lane), lds_addr

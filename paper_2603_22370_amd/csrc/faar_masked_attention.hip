@@ -602,8 +602,8 @@ __device__ __forceinline__ float with_low(uint32_t bf16_top, uint32_t byte) {
 
 // A workgroup: 128 queries of one head, 32 a wavefront (the columns of S^T = K Q^T, so that a lane holds scores of one query), and the blocks
 // of 64 keys that any of them sees.  Matrix cores and vector unit share a SIMD's issue (a product of 32 cycles takes 16 of it), and
-// the chip its power: 16384 tokens behind a prefix, 16 / 8 heads of 128, capped: 1190-1240 us, 0.9-0.94 PFLOP/s of what the masks leave (products
-// and LDS alone 836).  24 documents in 8192 tokens: 50 us, by the first loads of short items.
+// the chip its power: 16384 tokens behind a prefix, 16 / 8 heads of 128, capped: 1205-1240 us (1250 and more before the clock has settled), 0.9-0.93 PFLOP/s of
+// what the masks leave (products and LDS alone 836).  24 documents in 8192 tokens: 50 us, by the first loads of short items.
 template <class H, int kMode>
 __global__ void __launch_bounds__(256, 2)
 k_masked_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const int* __restrict__ plan, PlanTag tag,
@@ -819,7 +819,7 @@ __device__ __forceinline__ void masked_dq_tile(f32x16 (&acc)[H::DT], const bf16x
 }
 
 // The forward's split, walked again: S and dP = V dO^T in tiles of 32 keys, dq^T += K^T dz^T.  Bound like the forward, by a query's four operands
-// on short sequences: 8192 causal tokens, 16 / 8 heads of 128, 375 us (scores of deviation 1) to 428 (9), 485 capped; 24 documents
+// on short sequences: 8192 causal tokens, 16 / 8 heads of 128, 374 us (scores of deviation 1) to 423 (9), 479 capped; 24 documents
 // of 8192 tokens 71, of which vector unit 27 and matrix cores 13.
 template <class H, int kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
@@ -1002,7 +1002,7 @@ __device__ __forceinline__ void masked_dkv_tile(f32x16 (&dk)[H::DT], f32x16 (&dv
 // 64 keys of a key / value head a workgroup: wavefronts 0, 2 the first 32 and 1, 3 the others; 0, 1 take the first 32 queries of every
 // block of 64 and 2, 3 the others, and the two sums of a block of keys meet through LDS at the end.  All query heads of the group are walked,
 // so that no sum leaves the workgroup.  K, V, dk and dv take the registers of two wavefronts a SIMD (three with heads of 64: 13 images of
-// 10007 patches 153 us, with two 172).  8192 causal tokens, 16 / 8 heads of 128: 528 us (scores of deviation 1) to 633 (9), 645 capped.
+// 10007 patches 153 us, with two 172).  8192 causal tokens, 16 / 8 heads of 128: 527 us (scores of deviation 1) to 620 (9), 639 capped.
 template <class H, int kCap, bool kBias>
 __global__ void __launch_bounds__(256, 2)
 k_masked_bwd_dkv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,

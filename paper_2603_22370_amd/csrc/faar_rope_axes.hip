@@ -7,7 +7,7 @@
 //
 // HBM-bound (2 bytes in, 2 out an element), provided that the 64-bit products, the sine and the cosine are not taken per element:
 // a workgroup makes those of its tokens once, into LDS, and applies them to all heads of q and k.  201 MB (16384 tokens, 16 + 8
-// heads of 128) in 40 us, the rate of a large copy; 24 tokens take 2.6 us on the device.
+// heads of 128) in 40 us, the rate of a large copy (31 us where a part of them is still in the chip's cache); 24 tokens take 2.6 us on the device.
 #include "faar_internal.h"
 
 namespace faar {
